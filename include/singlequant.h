@@ -275,6 +275,132 @@ sq_status_t sq_linear_grouped(const sq_rotation_t* const* rots, int32_t E, const
                               const void* X, const void* const* Wq, const void* const* sw, int64_t N, int64_t K,
                               void* workspace, size_t workspace_bytes, void* Y, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Weight-only layers with group scales, and the sparse (mixture-of-experts) block around them.
+ * (The paper has no counterpart: 4-bit checkpoints keep one step per `group` input channels instead of
+ * one per output channel, and a sparse block needs its rows sorted by expert and brought back.)
+ *
+ *   w[c, k] = code[c, k] * sg[k / group, c] + bg[k / group, c]
+ *
+ *   codes  4 bits (or 3 in a nibble) in the weight-only order, uint8 [N x K/2], as sq_pack_weight_wo
+ *   group  32, 64 or 128 input channels (SQ_ERR_INVALID_ARG otherwise); G = ceil(K / group), the last
+ *          group may be short
+ *   sg     fp16 [G x N], group-major: the scales of all channels of one group lie side by side
+ *   bg     fp16 [G x N] or NULL (no offset).  A checkpoint with unsigned codes u and zero points z,
+ *          w = s (u - z), has code = u - 8 (u ^ 8 as a nibble) and bg = s (8 - z).
+ * sg and bg are finite and |code * sg + bg| < 65504: the kernels that multiply on the tensor cores round
+ * each weight once to fp16 (one fused multiply-add), the others keep it in fp32.  Sums are fp32.
+ * ------------------------------------------------------------------------------------------- */
+
+/* Offline: rotate the rows of W (fp32), quantise each group, store in the weight-only order.
+ *   rot_or_null   NULL = identity rotation (no workspace needed then)
+ *   W             DEVICE fp16 [N x K], K == n of the handle, K % 8 == 0, K <= 32768
+ *   bits          4 or 3
+ *   Wq, sg        DEVICE (out)
+ *   bg_or_null    NULL: symmetric, step = fp16(max|w| / (2^(bits-1) - 1)), code = clamp(floor(w / step + 1/2));
+ *                 else DEVICE (out): step = fp16((max - min) / (2^bits - 1)), offset = fp16(min + 2^(bits-1) step),
+ *                 code = clamp(floor((w - offset) / step + 1/2))
+ *   workspace     DEVICE, sq_pack_weight_gs_workspace_bytes(N, K) bytes, 256-byte aligned; unused with NULL rot */
+size_t sq_pack_weight_gs_workspace_bytes(int64_t N, int64_t K);
+sq_status_t sq_pack_weight_gs(const sq_rotation_t* rot_or_null, const void* W, int64_t N, int64_t K, int32_t bits,
+                              int32_t group, void* Wq, void* sg, void* bg_or_null, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* Y[t,c] = fp16(sum_k Z16[t,k] * w[c,k]).
+ *   Z16 DEVICE fp16 [M x K]     Wq, sg, bg as above     Y DEVICE fp16 [M x N] (out)
+ * K % 8 == 0, K <= 65536.  The fast kernels take K % 32 == 0 with N even up to 16 tokens, and K % 64 == 0 above;
+ * other shapes run a plain fp32 kernel.  The order of the sums is fixed for given M, N and K.  Ordering in the
+ * stream as sq_w4a4_gemm: Wq, sg and bg may be requested while the kernel before still runs. */
+sq_status_t sq_w4a16_gemm_gs(const void* Z16, const void* Wq, const void* sg, const void* bg_or_null, int64_t M,
+                             int64_t N, int64_t K, int32_t group, void* Y, void* stream);
+
+/* The layer: rotation into the workspace (sq_linear_wo_workspace_bytes(M, K) bytes, 256-byte aligned), then the
+ * product.  Every argument of both halves is validated before the first kernel is queued. */
+sq_status_t sq_linear_gs(const sq_rotation_t* rot, const void* X, int64_t M, const void* Wq, const void* sg,
+                         const void* bg_or_null, int64_t N, int64_t K, int32_t group, void* workspace,
+                         size_t workspace_bytes, void* Y, void* stream);
+
+/* The experts' products of a sparse block, with the routing on the device: for expert e and its rows
+ * offsets[e] <= r < offsets[e+1],
+ *   Y[r, c] = fp16(sum_k Z16[row_token[r], k] * w_e[c, k])
+ *   Z16               DEVICE fp16 [T x K]: the tokens, rotated once for all experts
+ *   row_token_or_null DEVICE int32 [M], or NULL: row r multiplies Z16's row r (T == M then).  A row whose token lies
+ *                     outside [0, T) counts as a row of zeros.
+ *   offsets           DEVICE int32 [E + 1], non-decreasing, offsets[0] == 0 (clamped to [0, M] where they are not)
+ *   E                 1 .. 1024 (SQ_ERR_UNSUPPORTED above)
+ *   Wq, sg, bg        as above, the experts one behind the other: [E x N x K/2], [E x G x N]
+ *   M                 rows that Y has room for; rows offsets[E] .. M-1 are left as they were
+ *   workspace         DEVICE, sq_gemm_gs_grouped_workspace_bytes(M, K) bytes (2 M K rounded up to 256), 256-byte
+ *                     aligned; calls that overlap on the GPU need one each
+ * Nothing is read back: the call may be captured, and a replay uses the routing that it finds. */
+size_t sq_gemm_gs_grouped_workspace_bytes(int64_t M, int64_t K);
+sq_status_t sq_w4a16_gemm_gs_grouped(const void* Z16, int64_t T, const void* row_token_or_null, const void* offsets,
+                                     int32_t E, const void* Wq, const void* sg, const void* bg_or_null, int64_t M,
+                                     int64_t N, int64_t K, int32_t group, void* workspace, size_t workspace_bytes,
+                                     void* Y, void* stream);
+
+/* The experts' layers: the T tokens are rotated once (all experts share `rot`), then the products.
+ *   X          DEVICE fp16 [T x K]
+ *   workspace  DEVICE, sq_linear_gs_grouped_workspace_bytes(T, M, K) bytes, 256-byte aligned */
+size_t sq_linear_gs_grouped_workspace_bytes(int64_t T, int64_t M, int64_t K);
+sq_status_t sq_linear_gs_grouped(const sq_rotation_t* rot, const void* X, int64_t T, const void* row_token_or_null,
+                                 const void* offsets, int32_t E, const void* Wq, const void* sg, const void* bg_or_null,
+                                 int64_t M, int64_t N, int64_t K, int32_t group, void* workspace,
+                                 size_t workspace_bytes, void* Y, void* stream);
+
+/* Types of the router's logits. */
+enum { SQ_F16 = 0, SQ_BF16 = 1, SQ_F32 = 2 };
+/* Gates are the softmax over the selected experts only (else over all E). */
+#define SQ_ROUTE_RENORM 1u
+
+/* The router of a sparse block.  For every token t with p = softmax(logits[t]): the k experts with the largest
+ * logits, largest first, the lower index first among equal ones; their gates; the rows sorted by expert, and by
+ * token within an expert; the balance loss
+ *   loss = E * sum_e (counts[e] / (k n)) * (sum_t p[t,e] / n),   n = number of tokens that count (0 if none does).
+ *   logits        DEVICE, `dtype` [T x E], row stride `ld` elements (ld >= E)
+ *   E             1 .. 1024, k 1 .. min(E, 32) (SQ_ERR_UNSUPPORTED above)
+ *   mask_or_null  DEVICE uint8 [T]: tokens with 0 are padding
+ *   ids           DEVICE int32 [T x k] (out)     gates  DEVICE fp32 [T x k] (out)
+ *   counts        DEVICE int32 [E + 1] (out): rows of every expert, and n behind them
+ *   offsets       DEVICE int32 [E + 1] (out): expert e owns rows offsets[e] .. offsets[e+1]-1
+ *   row_token     DEVICE int32 [T k] (out): the token of each row; entries from offsets[E] on are left as they were
+ *   pos           DEVICE int32 [T x k] (out): the row of each token's slot
+ *   loss_or_null  DEVICE fp32 [1] (out)
+ *   workspace     DEVICE, sq_route_workspace_bytes(T, E) bytes (at most 2 MB), 256-byte aligned
+ * An expert whose logit is -inf or NaN has p = 0 and is never selected; slots that are left over, and all slots of
+ * padding and of tokens without any usable logit (which do not count in n either), get id -1, gate 0, pos -1.
+ * Logits of +inf share p = 1.  T k < 2^31.  T = 0 writes counts, offsets and loss.  The results do not depend on the
+ * run: no atomics decide an order. */
+size_t sq_route_workspace_bytes(int64_t T, int32_t E);
+sq_status_t sq_route(const void* logits, int32_t dtype, int64_t T, int32_t E, int64_t ld, int32_t k, uint32_t flags,
+                     const void* mask_or_null, void* ids, void* gates, void* counts, void* offsets, void* row_token,
+                     void* pos, void* loss_or_null, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The gradient of sq_route with respect to the logits: of sum(dgates * gates) + dloss * loss, the selection and the
+ * counts taken as constants.  ids, gates, counts: what sq_route wrote for the same logits and flags.
+ *   dgates_or_null  DEVICE fp32 [T x k]; entries of slots with id -1 are not used
+ *   dloss_or_null   DEVICE fp32 [1]
+ *   dlogits         DEVICE, `dtype` [T x E], row stride ld_d (out; columns E .. ld_d-1 are left as they were; zeros for
+ *                   tokens that do not count; may be the logits themselves when ld_d == ld) */
+sq_status_t sq_route_backward(const void* logits, int32_t dtype, int64_t T, int32_t E, int64_t ld, int32_t k,
+                              uint32_t flags, const void* mask_or_null, const void* ids, const void* gates,
+                              const void* counts, const void* dgates_or_null, const void* dloss_or_null, void* dlogits,
+                              int64_t ld_d, void* stream);
+
+/* Back from expert rows to tokens: out[t] = fp16(sum_j gates[t,j] * Y[pos[t,j]]), in fp32 in the order of the slots.
+ * A slot whose pos lies outside [0, M) adds nothing; a token without slots gets zeros.
+ *   Y    DEVICE fp16 [M x N]     pos  DEVICE int32 [T x k]     gates  DEVICE fp32 [T x k]
+ *   out  DEVICE fp16 [T x N] (out; may not overlap Y)     k 1 .. 32 */
+sq_status_t sq_combine(const void* Y, int64_t M, const void* pos, const void* gates, int64_t T, int32_t k, int64_t N,
+                       void* out, void* stream);
+
+/* Its gradient: dY[pos[t,j]] = fp16(gates[t,j] * dout[t]), dgates[t,j] = sum_c dout[t,c] * Y[pos[t,j],c] (0 for slots
+ * without a row).  Every row belongs to one slot at most, as sq_route makes them; rows of dY that no slot names are
+ * left as they were.  Either output may be NULL.
+ *   dout  DEVICE fp16 [T x N]     dY_or_null  DEVICE fp16 [M x N] (out)     dgates_or_null  DEVICE fp32 [T x k] (out) */
+sq_status_t sq_combine_backward(const void* dout, const void* Y, int64_t M, const void* pos, const void* gates, int64_t T,
+                                int32_t k, int64_t N, void* dY_or_null, void* dgates_or_null, void* stream);
+
 /* Synchronises `stream`, then returns and clears the device status word: SQ_OK, or
  * SQ_ERR_TIMEOUT if any kernel since the last call gave up a bounded wait, or SQ_ERR_CUDA. */
 sq_status_t sq_last_device_status(void* stream);

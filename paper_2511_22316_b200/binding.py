@@ -23,6 +23,8 @@ SQ_ERR_NOMEM, SQ_ERR_CUDA, SQ_ERR_TIMEOUT = 5, 6, 7
 SQ_ROT_ART, SQ_ROT_URT, SQ_ROT_HADAMARD, SQ_ROT_DEFAULT = 1, 2, 4, 7
 SQ_ROT_APPLY_STRUCTURED = 1 << 20
 SQ_ROT_FUSE_DECODE = 1 << 21
+SQ_F16, SQ_BF16, SQ_F32 = 0, 1, 2
+SQ_ROUTE_RENORM = 1
 
 EXPORTS = (
     "sq_factorize", "sq_build_rotation", "sq_rotation_from_factors", "sq_rotation_get_factors",
@@ -32,6 +34,10 @@ EXPORTS = (
     "sq_debug_bounded_wait", "sq_kernel_launch_count", "sq_status_string",
     "sq_pack_weight_wo", "sq_rotate_act_f16", "sq_w4a16_gemm", "sq_linear_wo_workspace_bytes", "sq_linear_wo",
     "sq_linear_grouped",
+    "sq_pack_weight_gs_workspace_bytes", "sq_pack_weight_gs", "sq_w4a16_gemm_gs", "sq_linear_gs",
+    "sq_gemm_gs_grouped_workspace_bytes", "sq_w4a16_gemm_gs_grouped", "sq_linear_gs_grouped_workspace_bytes",
+    "sq_linear_gs_grouped", "sq_route_workspace_bytes", "sq_route", "sq_route_backward", "sq_combine",
+    "sq_combine_backward",
 )
 
 
@@ -86,6 +92,23 @@ def load() -> ctypes.CDLL:
                                  c_void_p, c_size_t, c_void_p, c_void_p]
     lib.sq_linear_grouped.argtypes = [POINTER(c_void_p), c_int32, POINTER(c_int64), c_void_p, POINTER(c_void_p),
                                       POINTER(c_void_p), c_int64, c_int64, c_void_p, c_size_t, c_void_p, c_void_p]
+    P, i32, i64 = c_void_p, c_int32, c_int64
+    lib.sq_pack_weight_gs_workspace_bytes.argtypes = [i64, i64]
+    lib.sq_pack_weight_gs.argtypes = [P, P, i64, i64, i32, i32, P, P, P, P, c_size_t, P]
+    lib.sq_w4a16_gemm_gs.argtypes = [P, P, P, P, i64, i64, i64, i32, P, P]
+    lib.sq_linear_gs.argtypes = [P, P, i64, P, P, P, i64, i64, i32, P, c_size_t, P, P]
+    lib.sq_gemm_gs_grouped_workspace_bytes.argtypes = [i64, i64]
+    lib.sq_w4a16_gemm_gs_grouped.argtypes = [P, i64, P, P, i32, P, P, P, i64, i64, i64, i32, P, c_size_t, P, P]
+    lib.sq_linear_gs_grouped_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.sq_linear_gs_grouped.argtypes = [P, P, i64, P, P, i32, P, P, P, i64, i64, i64, i32, P, c_size_t, P, P]
+    lib.sq_route_workspace_bytes.argtypes = [i64, i32]
+    lib.sq_route.argtypes = [P, i32, i64, i32, i64, i32, c_uint32, P, P, P, P, P, P, P, P, P, c_size_t, P]
+    lib.sq_route_backward.argtypes = [P, i32, i64, i32, i64, i32, c_uint32, P, P, P, P, P, P, P, i64, P]
+    lib.sq_combine.argtypes = [P, i64, P, P, i64, i32, i64, P, P]
+    lib.sq_combine_backward.argtypes = [P, P, i64, P, P, i64, i32, i64, P, P, P]
+    for name in ("sq_pack_weight_gs_workspace_bytes", "sq_gemm_gs_grouped_workspace_bytes",
+                 "sq_linear_gs_grouped_workspace_bytes", "sq_route_workspace_bytes"):
+        getattr(lib, name).restype = c_size_t
     lib.sq_last_device_status.argtypes = [c_void_p]
     lib.sq_debug_bounded_wait.argtypes = [c_uint32, c_void_p]
     lib.sq_kernel_launch_count.argtypes = []
@@ -295,6 +318,80 @@ def sq_linear_grouped(rots, offsets, X, Wq, sw, N: int, K: int, workspace, works
     sws = (c_void_p * E)(*[_ptr(w) for w in sw])
     _check(load().sq_linear_grouped(h, E, off, _ptr(X), wq, sws, N, K, _ptr(workspace), workspace_bytes, _ptr(Y),
                                     _stream(stream)), "sq_linear_grouped")
+
+
+def sq_pack_weight_gs_workspace_bytes(N: int, K: int) -> int:
+    return int(load().sq_pack_weight_gs_workspace_bytes(N, K))
+
+
+def sq_pack_weight_gs(rot: Optional[Rotation], W, N: int, K: int, bits: int, group: int, Wq, sg, bg=None, workspace=None,
+                      workspace_bytes: int = 0, stream=None) -> None:
+    """Offline weight path with group scales: symmetric, or with offsets when `bg` is given.  `sg`, `bg`: fp16 [G x N]."""
+    _check(load().sq_pack_weight_gs(None if rot is None else rot.handle, _ptr(W), N, K, int(bits), group, _ptr(Wq),
+                                    _ptr(sg), _ptr(bg), _ptr(workspace), workspace_bytes, _stream(stream)),
+           "sq_pack_weight_gs")
+
+
+def sq_w4a16_gemm_gs(Z16, Wq, sg, bg, M: int, N: int, K: int, group: int, Y, stream=None) -> None:
+    _check(load().sq_w4a16_gemm_gs(_ptr(Z16), _ptr(Wq), _ptr(sg), _ptr(bg), M, N, K, group, _ptr(Y), _stream(stream)),
+           "sq_w4a16_gemm_gs")
+
+
+def sq_linear_gs(rot: Rotation, X, M: int, Wq, sg, bg, N: int, K: int, group: int, workspace, workspace_bytes: int, Y,
+                 stream=None) -> None:
+    _check(load().sq_linear_gs(rot.handle, _ptr(X), M, _ptr(Wq), _ptr(sg), _ptr(bg), N, K, group, _ptr(workspace),
+                               workspace_bytes, _ptr(Y), _stream(stream)), "sq_linear_gs")
+
+
+def sq_gemm_gs_grouped_workspace_bytes(M: int, K: int) -> int:
+    return int(load().sq_gemm_gs_grouped_workspace_bytes(M, K))
+
+
+def sq_w4a16_gemm_gs_grouped(Z16, T: int, row_token, offsets, E: int, Wq, sg, bg, M: int, N: int, K: int, group: int,
+                             workspace, workspace_bytes: int, Y, stream=None) -> None:
+    """The experts' products on rows that `sq_route` sorted: `row_token` and `offsets` are its DEVICE outputs."""
+    _check(load().sq_w4a16_gemm_gs_grouped(_ptr(Z16), T, _ptr(row_token), _ptr(offsets), E, _ptr(Wq), _ptr(sg), _ptr(bg),
+                                           M, N, K, group, _ptr(workspace), workspace_bytes, _ptr(Y), _stream(stream)),
+           "sq_w4a16_gemm_gs_grouped")
+
+
+def sq_linear_gs_grouped_workspace_bytes(T: int, M: int, K: int) -> int:
+    return int(load().sq_linear_gs_grouped_workspace_bytes(T, M, K))
+
+
+def sq_linear_gs_grouped(rot: Rotation, X, T: int, row_token, offsets, E: int, Wq, sg, bg, M: int, N: int, K: int,
+                         group: int, workspace, workspace_bytes: int, Y, stream=None) -> None:
+    _check(load().sq_linear_gs_grouped(rot.handle, _ptr(X), T, _ptr(row_token), _ptr(offsets), E, _ptr(Wq), _ptr(sg),
+                                       _ptr(bg), M, N, K, group, _ptr(workspace), workspace_bytes, _ptr(Y),
+                                       _stream(stream)), "sq_linear_gs_grouped")
+
+
+def sq_route_workspace_bytes(T: int, E: int) -> int:
+    return int(load().sq_route_workspace_bytes(T, E))
+
+
+def sq_route(logits, dtype: int, T: int, E: int, ld: int, k: int, flags: int, mask, ids, gates, counts, offsets, row_token,
+             pos, loss, workspace, workspace_bytes: int, stream=None) -> None:
+    """The router: `dtype` is SQ_F16, SQ_BF16 or SQ_F32, `ld` the logits' row stride in elements; `mask` and `loss` may be None."""
+    _check(load().sq_route(_ptr(logits), dtype, T, E, ld, k, flags, _ptr(mask), _ptr(ids), _ptr(gates), _ptr(counts),
+                           _ptr(offsets), _ptr(row_token), _ptr(pos), _ptr(loss), _ptr(workspace), workspace_bytes,
+                           _stream(stream)), "sq_route")
+
+
+def sq_route_backward(logits, dtype: int, T: int, E: int, ld: int, k: int, flags: int, mask, ids, gates, counts, dgates, dloss,
+                      dlogits, ld_d: int, stream=None) -> None:
+    _check(load().sq_route_backward(_ptr(logits), dtype, T, E, ld, k, flags, _ptr(mask), _ptr(ids), _ptr(gates),
+                                    _ptr(counts), _ptr(dgates), _ptr(dloss), _ptr(dlogits), ld_d, _stream(stream)),
+           "sq_route_backward")
+
+
+def sq_combine(Y, M: int, pos, gates, T: int, k: int, N: int, out, stream=None) -> None:
+    _check(load().sq_combine(_ptr(Y), M, _ptr(pos), _ptr(gates), T, k, N, _ptr(out), _stream(stream)), "sq_combine")
+
+
+def sq_combine_backward(dout, Y, M: int, pos, gates, T: int, k: int, N: int, dY, dgates, stream=None) -> None:
+    _check(load().sq_combine_backward(_ptr(dout), _ptr(Y), M, _ptr(pos), _ptr(gates), T, k, N, _ptr(dY), _ptr(dgates),
+                                      _stream(stream)), "sq_combine_backward")
 
 
 def sq_last_device_status(stream=None) -> int:

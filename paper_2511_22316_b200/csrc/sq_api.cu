@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <vector>
 #include <new>
@@ -663,6 +664,234 @@ sq_status_t sq_linear_grouped(const sq_rotation_t* const* rots, int32_t E, const
     if (st != SQ_OK) return st;
   }
   return SQ_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Group scales and the sparse block
+// ---------------------------------------------------------------------------------------------
+namespace {
+constexpr int64_t kPackChunk = 1024;      // rows that sq_pack_weight_gs rotates at a time
+constexpr int32_t kMaxExperts = 1024, kMaxTopK = 32;
+
+bool group_ok(int32_t group) { return group == 32 || group == 64 || group == 128; }
+
+sq_status_t check_gs_args(const void* Z16, int64_t T, const void* Wq, const void* sg, const void* bg, int64_t M, int64_t N, int64_t K,
+                          int32_t group, const void* Y) {
+  if (T < 0 || M < 0 || N < 0 || T > kMaxRows || M > kMaxRows || N > kMaxRows || !group_ok(group)) return SQ_ERR_INVALID_ARG;
+  if (K < 8 || (K % 8) != 0) return SQ_ERR_SHAPE;
+  if (K > kMaxK) return SQ_ERR_UNSUPPORTED;
+  if (M == 0 || N == 0) return SQ_OK;
+  if (!Z16 || !Wq || !sg || !Y) return SQ_ERR_INVALID_ARG;
+  if (!sq::aligned16(Z16) || !sq::aligned16(Wq) || !sq::aligned16(sg) || !sq::aligned16(bg) || !sq::aligned16(Y)) return SQ_ERR_ALIGN;
+  return SQ_OK;
+}
+
+sq_status_t check_workspace(const void* workspace, size_t have, size_t need) {
+  if (need == 0) return SQ_OK;
+  if (!workspace) return SQ_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return SQ_ERR_ALIGN;
+  return have < need ? SQ_ERR_NOMEM : SQ_OK;
+}
+
+sq_status_t check_gs_grouped_args(const void* Z16, int64_t T, const void* row_token, const void* offsets, int32_t E, const void* Wq,
+                                  const void* sg, const void* bg, int64_t M, int64_t N, int64_t K, int32_t group, const void* Y) {
+  if (E < 1) return SQ_ERR_INVALID_ARG;
+  if (E > kMaxExperts) return SQ_ERR_UNSUPPORTED;
+  sq_status_t st = check_gs_args(Z16, T, Wq, sg, bg, M, N, K, group, Y);
+  if (st != SQ_OK || M == 0 || N == 0) return st;
+  if (!offsets || T < 1) return SQ_ERR_INVALID_ARG;
+  if (!row_token && T != M) return SQ_ERR_SHAPE;
+  if (!sq::aligned16(row_token) || !sq::aligned16(offsets)) return SQ_ERR_ALIGN;
+  return SQ_OK;
+}
+
+sq::GsArgs gs_args(const void* Z16, int64_t T, const void* row_token, const void* offsets, int32_t E, const void* Wq, const void* sg,
+                   const void* bg, int64_t M, int64_t N, int64_t K, int32_t group, void* Y) {
+  sq::GsArgs a;
+  a.Z = static_cast<const __half*>(Z16);
+  a.Wq = static_cast<const uint8_t*>(Wq);
+  a.sg = static_cast<const __half*>(sg);
+  a.bg = static_cast<const __half*>(bg);
+  a.row_token = static_cast<const int32_t*>(row_token);
+  a.offsets = static_cast<const int32_t*>(offsets);
+  a.Y = static_cast<__half*>(Y);
+  a.T = T;
+  a.M = M;
+  a.N = N;
+  a.K = static_cast<int>(K);
+  a.group = group;
+  a.E = E;
+  return a;
+}
+}  // namespace
+
+// Workspace layout of sq_pack_weight_gs: [rotated rows, fp32][codes and steps that the rotate kernels write besides].
+size_t sq_pack_weight_gs_workspace_bytes(int64_t N, int64_t K) {
+  if (N <= 0 || K <= 0 || N > kMaxRows || K > kMaxN) return 0;
+  const size_t rows = static_cast<size_t>(std::min(N, kPackChunk));
+  return align_up(rows * K * 4, 256) + align_up(rows * (K / 2), 256) + align_up(rows * 2, 256);
+}
+
+sq_status_t sq_pack_weight_gs(const sq_rotation_t* rot_or_null, const void* W, int64_t N, int64_t K, int32_t bits, int32_t group,
+                              void* Wq, void* sg, void* bg_or_null, void* workspace, size_t workspace_bytes, void* stream) {
+  if ((bits != 3 && bits != 4) || !group_ok(group)) return SQ_ERR_INVALID_ARG;
+  if (rot_or_null) {
+    if (static_cast<int64_t>(rot_or_null->n1) * rot_or_null->n2 != K) return SQ_ERR_SHAPE;
+    if (rot_or_null->n2 & 1) return SQ_ERR_SHAPE;
+  }
+  if (K < 8 || K % 8 != 0) return SQ_ERR_SHAPE;
+  sq_status_t st = check_rows_args(W, Wq, sg, bg_or_null, N, K);
+  if (st != SQ_OK || N == 0) return st;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (!rot_or_null)
+    return sq::launch_quant_groups(W, false, N, 0, N, static_cast<int>(K), group, bits, Wq, sg, bg_or_null, s);
+  if ((st = check_workspace(workspace, workspace_bytes, sq_pack_weight_gs_workspace_bytes(N, K))) != SQ_OK) return st;
+  if ((st = check_handle_device(rot_or_null)) != SQ_OK) return st;
+  const size_t rows = static_cast<size_t>(std::min(N, kPackChunk));
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  unsigned char* codes = ws + align_up(rows * K * 4, 256);
+  unsigned char* steps = codes + align_up(rows * (K / 2), 256);
+  for (int64_t r0 = 0; r0 < N && st == SQ_OK; r0 += kPackChunk) {
+    const int64_t r = std::min(N - r0, kPackChunk);
+    st = sq::rotate_quant_dispatch(rot_or_null, static_cast<const unsigned char*>(W) + static_cast<size_t>(r0) * K * 2, r, codes, steps,
+                                   reinterpret_cast<float*>(ws), s);
+    if (st == SQ_OK)
+      st = sq::launch_quant_groups(ws, true, r, r0, N, static_cast<int>(K), group, bits, Wq, sg, bg_or_null, s);
+  }
+  return st;
+}
+
+sq_status_t sq_w4a16_gemm_gs(const void* Z16, const void* Wq, const void* sg, const void* bg_or_null, int64_t M, int64_t N, int64_t K,
+                             int32_t group, void* Y, void* stream) {
+  sq_status_t st = check_gs_args(Z16, M, Wq, sg, bg_or_null, M, N, K, group, Y);
+  if (st != SQ_OK || M == 0 || N == 0) return st;
+  return sq::launch_gemm_gs(gs_args(Z16, M, nullptr, nullptr, 0, Wq, sg, bg_or_null, M, N, K, group, Y), nullptr,
+                            static_cast<cudaStream_t>(stream));
+}
+
+sq_status_t sq_linear_gs(const sq_rotation_t* rot, const void* X, int64_t M, const void* Wq, const void* sg, const void* bg_or_null,
+                         int64_t N, int64_t K, int32_t group, void* workspace, size_t workspace_bytes, void* Y, void* stream) {
+  if (!rot) return SQ_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(rot->n1) * rot->n2 != K) return SQ_ERR_SHAPE;
+  if (rot->n2 & 1) return SQ_ERR_SHAPE;
+  if (M < 0 || N < 0 || !group_ok(group)) return SQ_ERR_INVALID_ARG;
+  if (M == 0 || N == 0) return SQ_OK;
+  sq_status_t st = check_workspace(workspace, workspace_bytes, sq_linear_wo_workspace_bytes(M, K));
+  if (st != SQ_OK) return st;
+  if ((st = check_rows_args(X, workspace, workspace, nullptr, M, K)) != SQ_OK) return st;
+  if ((st = check_gs_args(workspace, M, Wq, sg, bg_or_null, M, N, K, group, Y)) != SQ_OK) return st;
+  if ((st = check_handle_device(rot)) != SQ_OK) return st;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((st = sq::rotate_f16_dispatch(rot, X, M, workspace, s)) != SQ_OK) return st;
+  return sq::launch_gemm_gs(gs_args(workspace, M, nullptr, nullptr, 0, Wq, sg, bg_or_null, M, N, K, group, Y), nullptr, s);
+}
+
+size_t sq_gemm_gs_grouped_workspace_bytes(int64_t M, int64_t K) { return sq_linear_wo_workspace_bytes(M, K); }
+
+sq_status_t sq_w4a16_gemm_gs_grouped(const void* Z16, int64_t T, const void* row_token_or_null, const void* offsets, int32_t E,
+                                     const void* Wq, const void* sg, const void* bg_or_null, int64_t M, int64_t N, int64_t K,
+                                     int32_t group, void* workspace, size_t workspace_bytes, void* Y, void* stream) {
+  sq_status_t st = check_gs_grouped_args(Z16, T, row_token_or_null, offsets, E, Wq, sg, bg_or_null, M, N, K, group, Y);
+  if (st != SQ_OK || M == 0 || N == 0) return st;
+  if ((st = check_workspace(workspace, workspace_bytes, sq_gemm_gs_grouped_workspace_bytes(M, K))) != SQ_OK) return st;
+  return sq::launch_gemm_gs(gs_args(Z16, T, row_token_or_null, offsets, E, Wq, sg, bg_or_null, M, N, K, group, Y), workspace,
+                            static_cast<cudaStream_t>(stream));
+}
+
+// Workspace layout of sq_linear_gs_grouped: [rotated tokens: 2 T K][the product's workspace].
+size_t sq_linear_gs_grouped_workspace_bytes(int64_t T, int64_t M, int64_t K) {
+  return sq_linear_wo_workspace_bytes(T, K) + sq_gemm_gs_grouped_workspace_bytes(M, K);
+}
+
+sq_status_t sq_linear_gs_grouped(const sq_rotation_t* rot, const void* X, int64_t T, const void* row_token_or_null, const void* offsets,
+                                 int32_t E, const void* Wq, const void* sg, const void* bg_or_null, int64_t M, int64_t N, int64_t K,
+                                 int32_t group, void* workspace, size_t workspace_bytes, void* Y, void* stream) {
+  if (!rot) return SQ_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(rot->n1) * rot->n2 != K) return SQ_ERR_SHAPE;
+  if (rot->n2 & 1) return SQ_ERR_SHAPE;
+  if (T < 0 || M < 0 || N < 0 || !group_ok(group) || E < 1) return SQ_ERR_INVALID_ARG;
+  if (M == 0 || N == 0) return SQ_OK;
+  sq_status_t st = check_workspace(workspace, workspace_bytes, sq_linear_gs_grouped_workspace_bytes(T, M, K));
+  if (st != SQ_OK) return st;
+  if ((st = check_rows_args(X, workspace, workspace, nullptr, T, K)) != SQ_OK) return st;
+  if ((st = check_gs_grouped_args(workspace, T, row_token_or_null, offsets, E, Wq, sg, bg_or_null, M, N, K, group, Y)) != SQ_OK)
+    return st;
+  if ((st = check_handle_device(rot)) != SQ_OK) return st;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((st = sq::rotate_f16_dispatch(rot, X, T, workspace, s)) != SQ_OK) return st;
+  return sq::launch_gemm_gs(gs_args(workspace, T, row_token_or_null, offsets, E, Wq, sg, bg_or_null, M, N, K, group, Y),
+                            static_cast<unsigned char*>(workspace) + sq_linear_wo_workspace_bytes(T, K), s);
+}
+
+namespace {
+sq_status_t check_route_args(const void* logits, int32_t dtype, int64_t T, int32_t E, int64_t ld, int32_t k, uint32_t flags) {
+  if (dtype < SQ_F16 || dtype > SQ_F32 || T < 0 || E < 1 || k < 1 || k > E || (flags & ~SQ_ROUTE_RENORM)) return SQ_ERR_INVALID_ARG;
+  if (E > kMaxExperts || k > kMaxTopK || T > kMaxRows / k) return SQ_ERR_UNSUPPORTED;
+  if (ld < E) return SQ_ERR_SHAPE;
+  if (T > 0 && !logits) return SQ_ERR_INVALID_ARG;
+  return SQ_OK;
+}
+bool all_aligned(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (!sq::aligned16(p)) return false;
+  return true;
+}
+}  // namespace
+
+size_t sq_route_workspace_bytes(int64_t T, int32_t E) {
+  if (T <= 0 || E <= 0 || E > kMaxExperts || T > kMaxRows) return 0;
+  return sq::route_workspace_bytes(T, E);
+}
+
+sq_status_t sq_route(const void* logits, int32_t dtype, int64_t T, int32_t E, int64_t ld, int32_t k, uint32_t flags,
+                     const void* mask_or_null, void* ids, void* gates, void* counts, void* offsets, void* row_token, void* pos,
+                     void* loss_or_null, void* workspace, size_t workspace_bytes, void* stream) {
+  sq_status_t st = check_route_args(logits, dtype, T, E, ld, k, flags);
+  if (st != SQ_OK) return st;
+  if (!counts || !offsets || (T > 0 && (!ids || !gates || !row_token || !pos))) return SQ_ERR_INVALID_ARG;
+  if (!all_aligned({logits, mask_or_null, ids, gates, counts, offsets, row_token, pos, loss_or_null})) return SQ_ERR_ALIGN;
+  if ((st = check_workspace(workspace, workspace_bytes, sq_route_workspace_bytes(T, E))) != SQ_OK) return st;
+  return sq::launch_route(logits, dtype, T, E, ld, k, (flags & SQ_ROUTE_RENORM) != 0, mask_or_null, ids, gates, counts, offsets,
+                          row_token, pos, loss_or_null, workspace, static_cast<cudaStream_t>(stream));
+}
+
+sq_status_t sq_route_backward(const void* logits, int32_t dtype, int64_t T, int32_t E, int64_t ld, int32_t k, uint32_t flags,
+                              const void* mask_or_null, const void* ids, const void* gates, const void* counts,
+                              const void* dgates_or_null, const void* dloss_or_null, void* dlogits, int64_t ld_d, void* stream) {
+  sq_status_t st = check_route_args(logits, dtype, T, E, ld, k, flags);
+  if (st != SQ_OK) return st;
+  if (ld_d < E) return SQ_ERR_SHAPE;
+  if (T == 0) return SQ_OK;
+  if (!ids || !gates || !counts || !dlogits || (dlogits == logits && ld_d != ld)) return SQ_ERR_INVALID_ARG;
+  if (!all_aligned({logits, mask_or_null, ids, gates, counts, dgates_or_null, dloss_or_null, dlogits})) return SQ_ERR_ALIGN;
+  return sq::launch_route_backward(logits, dtype, T, E, ld, k, (flags & SQ_ROUTE_RENORM) != 0, mask_or_null, ids, gates, counts,
+                                   dgates_or_null, dloss_or_null, dlogits, ld_d, static_cast<cudaStream_t>(stream));
+}
+
+namespace {
+sq_status_t check_combine_args(int64_t M, int64_t T, int32_t k, int64_t N) {
+  if (M < 0 || T < 0 || N < 0 || k < 1 || M > kMaxRows || T > kMaxRows || N > kMaxRows) return SQ_ERR_INVALID_ARG;
+  return k > kMaxTopK || T > kMaxRows / k ? SQ_ERR_UNSUPPORTED : SQ_OK;
+}
+}  // namespace
+
+sq_status_t sq_combine(const void* Y, int64_t M, const void* pos, const void* gates, int64_t T, int32_t k, int64_t N, void* out,
+                       void* stream) {
+  sq_status_t st = check_combine_args(M, T, k, N);
+  if (st != SQ_OK || T == 0 || N == 0) return st;
+  if ((!Y && M > 0) || !pos || !gates || !out || out == Y) return SQ_ERR_INVALID_ARG;
+  if (!all_aligned({Y, pos, gates, out})) return SQ_ERR_ALIGN;
+  return sq::launch_combine(Y, M, pos, gates, T, k, N, out, static_cast<cudaStream_t>(stream));
+}
+
+sq_status_t sq_combine_backward(const void* dout, const void* Y, int64_t M, const void* pos, const void* gates, int64_t T, int32_t k,
+                                int64_t N, void* dY_or_null, void* dgates_or_null, void* stream) {
+  sq_status_t st = check_combine_args(M, T, k, N);
+  if (st != SQ_OK || T == 0 || (N == 0 && !dgates_or_null)) return st;
+  if (!dout || (!Y && M > 0) || !pos || !gates || (dY_or_null && (dY_or_null == Y || dY_or_null == dout))) return SQ_ERR_INVALID_ARG;
+  if (!all_aligned({dout, Y, pos, gates, dY_or_null, dgates_or_null})) return SQ_ERR_ALIGN;
+  if (!dY_or_null && !dgates_or_null) return SQ_OK;
+  return sq::launch_combine_backward(dout, Y, M, pos, gates, T, k, N, dY_or_null, dgates_or_null, static_cast<cudaStream_t>(stream));
 }
 
 sq_status_t sq_last_device_status(void* stream) {

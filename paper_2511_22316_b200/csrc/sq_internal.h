@@ -1,5 +1,6 @@
 // Internal declarations shared by the translation units of libsinglequant.
 #pragma once
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -207,6 +208,34 @@ sq_status_t launch_wo_gemm(const void* Z16, const void* Wq, const void* sw, int6
                            cudaStream_t s);
 // Rewrites packed rows [rows x K/2] from channel order into the weight-only storage order, in place.
 sq_status_t launch_interleave_nibbles(void* Wq, int64_t rows, int64_t K, cudaStream_t s);
+
+// Weight-only products with group scales (sq_gemm_gs.cu).
+struct GsArgs {
+  const __half* Z;                 // [T x K]
+  const uint8_t* Wq;               // [experts x N x K/2]
+  const __half *sg, *bg;           // [experts x G x N]; bg may be null
+  const int32_t *row_token, *offsets;      // null / null: dense
+  __half* Y;                       // [M x N]
+  int64_t T, M, N;
+  int K, group, E;                 // E = 0: dense
+};
+sq_status_t launch_gemm_gs(const GsArgs& a, void* workspace, cudaStream_t s);
+// `rows` rows of X (fp16 or fp32, [rows x K]) are rows row0 .. of a weight matrix of N channels.
+sq_status_t launch_quant_groups(const void* X, bool f32, int64_t rows, int64_t row0, int64_t N, int K, int group, int bits, void* Wq,
+                                void* sg, void* bg, cudaStream_t s);
+
+// The router and the combination of a sparse block (sq_route.cu).
+size_t route_workspace_bytes(int64_t T, int32_t E);
+sq_status_t launch_route(const void* logits, int dtype, int64_t T, int E, int64_t ld, int k, bool renorm, const void* mask, void* ids,
+                         void* gates, void* counts, void* offsets, void* row_token, void* pos, void* loss, void* workspace,
+                         cudaStream_t s);
+sq_status_t launch_route_backward(const void* logits, int dtype, int64_t T, int E, int64_t ld, int k, bool renorm, const void* mask,
+                                  const void* ids, const void* gates, const void* counts, const void* dgates, const void* dloss,
+                                  void* dlogits, int64_t ld_d, cudaStream_t s);
+sq_status_t launch_combine(const void* Y, int64_t M, const void* pos, const void* gates, int64_t T, int k, int64_t N, void* out,
+                           cudaStream_t s);
+sq_status_t launch_combine_backward(const void* dout, const void* Y, int64_t M, const void* pos, const void* gates, int64_t T, int k,
+                                    int64_t N, void* dY, void* dgates, cudaStream_t s);
 
 // Device status word helpers (sq_api.cu).
 sq_status_t read_and_clear_device_status(cudaStream_t s);

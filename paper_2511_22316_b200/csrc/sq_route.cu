@@ -1,0 +1,806 @@
+// The router of a sparse block and the way back from its experts' rows to tokens.
+//   route_kernel / route_finish_kernel   softmax, top-k, gates, rows sorted by expert, per-expert counts, balance loss
+//   route_backward_kernel                the gradient with respect to the logits
+//   combine_kernel / combine_backward_kernel
+//
+// With p = softmax(l): gates g_j = p of the j-th largest logit, or p_j over the sum of the selected ones; loss =
+// E sum_e f_e P_e with f_e = counts_e / (k n), P_e = sum_t p_te / n.  With c_e = dloss E f_e / n:
+//   dl = p (d - sum_e p_e d_e),  d_e = c_e  (+ dgates_j where e is the token's j-th expert, gates over all experts)
+//   dl_{e_j} += g_j (dgates_j - sum_i g_i dgates_i)   (gates over the selected experts)
+//
+// All of it is bound by memory where there are many tokens and by latency where there are few.  A token belongs to LPT lanes of
+// a warp (8, 16 or 32), EPL neighbouring experts to each of them: a row is one vector load per lane, stays in registers, and
+// ties go to the lowest lane and so to the lowest index.  Every group of LPT lanes takes a contiguous run of tokens, and every
+// block a run of groups: the row that a slot gets is the number of slots of the same expert before it, and that is the sum of
+// counts per block, per group and within the group, with no atomics whose order could matter.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "sq_internal.h"
+#include "sq_ptx.cuh"
+
+namespace sq {
+namespace {
+
+constexpr int RT_THREADS = 512;
+constexpr int RT_MAX_BLOCKS = 148;                   // the second kernel reads every block's counts
+constexpr uint32_t RT_KEY_NINF = 0x007FFFFFu;        // route_key(-inf): not above it is not usable
+constexpr float RT_NINF = -__builtin_huge_valf();
+
+struct RouteArgs {
+  const void* logits;
+  int dtype;
+  int E, k;
+  long long T, ld;
+  int renorm;
+  int vec;                                           // a lane's experts may be read as whole 4, 8 or 16-byte pieces
+  const uint8_t* mask;
+};
+
+__device__ __forceinline__ float bits_to_float(uint32_t h, int dtype) {
+  return dtype == SQ_F16 ? __half2float(__ushort_as_half(static_cast<unsigned short>(h))) : __uint_as_float(h << 16);
+}
+
+// The EPL logits of this lane: experts lane * EPL .. + EPL - 1; -inf behind the last expert and for NaN.
+template <int LPT, int EPL>
+__device__ __forceinline__ void route_load(const RouteArgs& a, long long t, int sub, float (&x)[EPL]) {
+  const int e0 = sub * EPL;
+  const bool mine = e0 < a.E;
+  if (a.dtype == SQ_F32) {
+    const float* row = static_cast<const float*>(a.logits) + t * a.ld + e0;
+    if (EPL % 4 == 0 && a.vec) {
+#pragma unroll
+      for (int i = 0; i < EPL / 4; ++i) {
+        const float4 v = mine ? *reinterpret_cast<const float4*>(row + 4 * i) : make_float4(RT_NINF, RT_NINF, RT_NINF, RT_NINF);
+        x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+      }
+    } else if (EPL == 2 && a.vec) {
+      const float2 v = mine ? *reinterpret_cast<const float2*>(row) : make_float2(RT_NINF, RT_NINF);
+      x[0] = v.x; x[EPL - 1] = v.y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) x[i] = e0 + i < a.E ? row[i] : RT_NINF;
+    }
+  } else {
+    const unsigned short* row = static_cast<const unsigned short*>(a.logits) + t * a.ld + e0;
+    if (EPL % 8 == 0 && a.vec) {
+#pragma unroll
+      for (int i = 0; i < EPL / 8; ++i) {
+        const uint4 v = mine ? *reinterpret_cast<const uint4*>(row + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[8 * i + 2 * j] = mine ? bits_to_float(w[j] & 0xFFFFu, a.dtype) : RT_NINF;
+          x[8 * i + 2 * j + 1] = mine ? bits_to_float(w[j] >> 16, a.dtype) : RT_NINF;
+        }
+      }
+    } else if (EPL == 4 && a.vec) {
+      const uint2 v = mine ? *reinterpret_cast<const uint2*>(row) : make_uint2(0u, 0u);
+      const uint32_t w[2] = {v.x, v.y};
+#pragma unroll
+      for (int j = 0; j < EPL / 2; ++j) {
+        x[2 * j] = mine ? bits_to_float(w[j & 1] & 0xFFFFu, a.dtype) : RT_NINF;
+        x[2 * j + 1] = mine ? bits_to_float(w[j & 1] >> 16, a.dtype) : RT_NINF;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) x[i] = e0 + i < a.E ? bits_to_float(row[i], a.dtype) : RT_NINF;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) x[i] = x[i] != x[i] ? RT_NINF : x[i];
+}
+
+// Order of the selection as unsigned integers; 0 is below every logit's.  (+ 0: -0 and 0 are equal.)
+__device__ __forceinline__ uint32_t route_key(float x) {
+  const uint32_t u = __float_as_uint(x + 0.0f);
+  return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
+}
+// exp(x - m) for x <= m: 1 at x == m, infinite or not.
+__device__ __forceinline__ float route_exp(float x, float m) { return x == m ? 1.0f : expf(x - m); }
+
+template <int LPT>
+__device__ __forceinline__ float group_max(float v) {
+#pragma unroll
+  for (int o = LPT / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+  return v;
+}
+template <int LPT>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = LPT / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  return v;
+}
+
+// p of this lane's experts, and whether the token counts (a usable logit; the mask is the caller's).  All lanes of the warp.
+template <int LPT, int EPL>
+__device__ __forceinline__ bool route_softmax(const float (&x)[EPL], float (&p)[EPL], float& m, float& inv) {
+  m = x[0];
+#pragma unroll
+  for (int i = 1; i < EPL; ++i) m = fmaxf(m, x[i]);
+  m = group_max<LPT>(m);
+  const bool usable = m > RT_NINF;
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    p[i] = usable && x[i] > RT_NINF ? route_exp(x[i], m) : 0.0f;
+    s += p[i];
+  }
+  s = group_sum<LPT>(s);
+  inv = usable ? 1.0f / s : 0.0f;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) p[i] *= inv;
+  return usable;
+}
+
+// What one block of the second kernel, or the only block of the first, does with the counts of all blocks before it.
+__device__ __forceinline__ void route_place(const int* base, const int32_t* ids, int32_t* pos, int32_t* row_token, long long first,
+                                            long long last, int k) {
+  for (long long i = first * k + threadIdx.x; i < last * k; i += blockDim.x) {
+    const int id = ids[i];
+    if (id >= 0) {
+      const int r = pos[i] + base[id];
+      pos[i] = r;
+      row_token[r] = static_cast<int32_t>(i / k);
+    }
+  }
+}
+
+// Exclusive scan of v over the block's threads; `warp_sums`: 33 ints.  Returns the sum before this thread; total in warp_sums[32].
+__device__ __forceinline__ int block_scan(int v, int* warp_sums) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int s = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xFFFFFFFFu, s, o);
+    if (lane >= o) s += u;
+  }
+  __syncthreads();
+  if (lane == 31) warp_sums[warp] = s;
+  __syncthreads();
+  if (warp == 0) {
+    const int nw = blockDim.x >> 5;
+    int w = lane < nw ? warp_sums[lane] : 0;
+    const int own = w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xFFFFFFFFu, w, o);
+      if (lane >= o) w += u;
+    }
+    if (lane == 31) warp_sums[32] = w;
+    warp_sums[lane] = w - own;
+  }
+  __syncthreads();
+  return warp_sums[warp] + s - v;
+}
+
+__device__ __forceinline__ double block_sum(double v, double* sums) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  __syncthreads();
+  if (lane == 0) sums[warp] = v;
+  __syncthreads();
+  v = 0.0;
+  for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) v += sums[w];
+  return v;
+}
+
+// Shared memory: counters [groups][E] (int), base [E] (int) and, over the counters once they have been read, sums of p.
+template <int LPT, int EPL>
+__global__ void __launch_bounds__(RT_THREADS)
+route_kernel(const RouteArgs a, long long chunk, int32_t* __restrict__ ids, float* __restrict__ gates, int32_t* pos,
+             int32_t* __restrict__ hist, float* __restrict__ psum, int32_t* __restrict__ counts, int32_t* __restrict__ offsets,
+             int32_t* __restrict__ row_token, float* __restrict__ loss) {
+  constexpr int GROUPS = RT_THREADS / LPT;
+  griddep_launch_dependents();
+  extern __shared__ __align__(16) unsigned char rt_smem[];
+  int* cnt = reinterpret_cast<int*>(rt_smem);        // [GROUPS][E]
+  float* ps = reinterpret_cast<float*>(rt_smem) + static_cast<size_t>(GROUPS) * a.E;      // [GROUPS][E]
+  int* base = reinterpret_cast<int*>(ps + static_cast<size_t>(GROUPS) * a.E);             // [E]
+  __shared__ int warp_sums[33];
+  __shared__ double sums[32];
+  __shared__ int live_of[GROUPS];
+
+  const int grp = threadIdx.x / LPT, sub = threadIdx.x % LPT, lane = threadIdx.x & 31;
+  const int E = a.E, k = a.k;
+  for (int i = threadIdx.x; i < GROUPS * E; i += RT_THREADS) cnt[i] = 0;
+  __syncthreads();
+  griddep_wait();                                    // the logits come from, and the outputs may be read by, the kernel before
+
+  const long long first = blockIdx.x * chunk, last = first + chunk < a.T ? first + chunk : a.T;
+  const long long run = (chunk + GROUPS - 1) / GROUPS;
+  const long long t0 = first + grp * run, t1 = t0 + run < last ? t0 + run : last;
+  int* my_cnt = cnt + grp * E;
+  float acc[EPL], x[EPL], next[EPL];
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) { acc[i] = 0.0f; next[i] = RT_NINF; }
+  int live = 0;
+  if (t0 < t1) route_load<LPT, EPL>(a, t0, sub, next);
+  for (long long it = 0; it < run; ++it) {           // every group of a warp: the shuffles below are the warp's
+    const long long t = t0 + it;
+    const bool in = t < t1;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) x[i] = in ? next[i] : RT_NINF;
+    if (t + 1 < t1) route_load<LPT, EPL>(a, t + 1, sub, next);
+    if (in && a.mask != nullptr && a.mask[t] == 0) {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) x[i] = RT_NINF;
+    }
+    float p[EPL], m, inv;
+    live += route_softmax<LPT, EPL>(x, p, m, inv) ? 1 : 0;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) acc[i] += p[i];
+
+    // The k largest: the lane's own best first, then the best of the lanes; equal ones to the lowest index.
+    uint32_t key[EPL], best = 0;
+    int bi = 0;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      key[i] = route_key(x[i]);
+      if (key[i] > best) { best = key[i]; bi = i; }
+    }
+    int my_id = -1;
+    float my_e = 0.0f, ssel = 0.0f;
+    for (int j = 0; j < k; ++j) {
+      uint32_t top;
+      int winner;
+      if (LPT == 32) {
+        top = __reduce_max_sync(0xFFFFFFFFu, best);
+        winner = __ffs(__ballot_sync(0xFFFFFFFFu, best == top)) - 1;
+      } else {
+        top = best;
+#pragma unroll
+        for (int o = LPT / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        const uint32_t who = __ballot_sync(0xFFFFFFFFu, best == top) >> (lane & ~(LPT - 1) & 31);
+        winner = __ffs(who & (LPT == 32 ? 0xFFFFFFFFu : (1u << (LPT & 31)) - 1u)) - 1;
+      }
+      const int wi = __shfl_sync(0xFFFFFFFFu, bi, winner, LPT);
+      const bool usable = top > RT_KEY_NINF;
+      const float v = __uint_as_float(top & 0x80000000u ? top ^ 0x80000000u : ~top);      // the logit itself
+      const float ev = usable ? route_exp(v, m) : 0.0f;
+      ssel += ev;
+      if (sub == j) {
+        my_id = usable ? winner * EPL + wi : -1;
+        my_e = ev;
+      }
+      if (sub == winner) {
+        best = 0;
+        int nb = 0;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+          if (i == bi) key[i] = 0;
+          if (key[i] > best) { best = key[i]; nb = i; }
+        }
+        bi = nb;
+      }
+    }
+    if (in && sub < k) {
+      const long long o = t * k + sub;
+      ids[o] = my_id;
+      gates[o] = my_id >= 0 ? (a.renorm ? my_e / ssel : my_e * inv) : 0.0f;
+      int r = -1;
+      if (my_id >= 0) {                              // the token's experts differ: no two lanes share a counter
+        r = my_cnt[my_id];
+        my_cnt[my_id] = r + 1;
+      }
+      pos[o] = r;                                    // within the group, for now
+    }
+    __syncwarp();
+  }
+#pragma unroll
+  for (int i = 0; i < EPL; ++i)
+    if (sub * EPL + i < E) ps[grp * E + sub * EPL + i] = acc[i];
+  if (sub == 0) live_of[grp] = live;
+  __syncthreads();
+
+  // Counts of the groups before, and the block's own.
+  const bool only = gridDim.x == 1;
+  double part = 0.0;
+  int n = 0;
+  for (int g = 0; g < GROUPS; ++g) n += live_of[g];
+  int carry = 0;
+  for (int e0 = 0; e0 < E; e0 += RT_THREADS) {       // (uniform: block_scan is the whole block's)
+    const int e = e0 + threadIdx.x;
+    int c = 0;
+    float s = 0.0f;
+    if (e < E) {
+      for (int g = 0; g < GROUPS; ++g) {
+        const int v = cnt[g * E + e];
+        cnt[g * E + e] = c;
+        c += v;
+        s += ps[g * E + e];
+      }
+      if (!only) {
+        hist[static_cast<size_t>(blockIdx.x) * (E + 1) + e] = c;
+        psum[static_cast<size_t>(blockIdx.x) * E + e] = s;
+        base[e] = 0;
+      }
+    }
+    if (only) {
+      const int off = carry + block_scan(c, warp_sums);
+      carry += warp_sums[32];
+      if (e < E) {
+        base[e] = off;
+        counts[e] = c;
+        offsets[e] = off;
+        part += static_cast<double>(c) * s;
+      }
+    }
+  }
+  if (only) {
+    const double all = block_sum(part, sums);
+    if (threadIdx.x == 0) {
+      counts[E] = n;
+      offsets[E] = carry;
+      if (loss != nullptr) *loss = n > 0 ? static_cast<float>(all * E / (static_cast<double>(k) * n * n)) : 0.0f;
+    }
+  } else if (threadIdx.x == 0) {
+    hist[static_cast<size_t>(blockIdx.x) * (E + 1) + E] = n;
+  }
+  __syncthreads();
+  // The slots' rows within the block (or for good, and then the rows' tokens too).
+  for (long long i = t0 * k + sub; i < t1 * k; i += LPT) {
+    const int id = ids[i];
+    if (id >= 0) {
+      const int r = pos[i] + cnt[grp * E + id] + base[id];
+      pos[i] = r;
+      if (only) row_token[r] = static_cast<int32_t>(i / k);
+    }
+  }
+}
+
+// Blocks 0 .. B-1: the final rows of block b's tokens.  Block B: counts, offsets and the loss.
+__global__ void __launch_bounds__(1024)
+route_finish_kernel(int B, int E, int k, long long T, long long chunk, const int32_t* __restrict__ hist,
+                    const float* __restrict__ psum, const int32_t* __restrict__ ids, int32_t* pos, int32_t* __restrict__ counts,
+                    int32_t* __restrict__ offsets, int32_t* __restrict__ row_token, float* __restrict__ loss) {
+  griddep_launch_dependents();
+  extern __shared__ __align__(16) unsigned char rt_smem[];
+  int* before = reinterpret_cast<int*>(rt_smem);     // [parts][E]: counts of the blocks before this one
+  const int parts = max(1, 1024 / E);
+  int* total = before + parts * E;                   // [parts][E]
+  float* prob = reinterpret_cast<float*>(total + parts * E);      // [parts][E], the last block's
+  __shared__ int warp_sums[33];
+  __shared__ double sums[32];
+  griddep_wait();
+
+  const int b = blockIdx.x;
+  for (int i = threadIdx.x; i < parts * E; i += blockDim.x) {
+    const int e = i % E, part = i / E;
+    int s = 0, all = 0;
+    float q = 0.0f;
+    const int lo = part * B / parts, hi = (part + 1) * B / parts;
+#pragma unroll 8
+    for (int o = lo; o < hi; ++o) {
+      const int v = hist[static_cast<size_t>(o) * (E + 1) + e];
+      all += v;
+      s += o < b ? v : 0;
+    }
+    if (b == B) {
+#pragma unroll 8
+      for (int o = lo; o < hi; ++o) q += psum[static_cast<size_t>(o) * E + e];
+      prob[i] = q;
+    }
+    before[i] = s;
+    total[i] = all;
+  }
+  __syncthreads();
+  int carry = 0;
+  double part_loss = 0.0;
+  for (int e0 = 0; e0 < E; e0 += blockDim.x) {
+    const int e = e0 + threadIdx.x;
+    int s = 0, all = 0;
+    double q = 0.0;
+    if (e < E) {
+      for (int p = 0; p < parts; ++p) {
+        s += before[p * E + e];
+        all += total[p * E + e];
+        if (b == B) q += prob[p * E + e];
+      }
+    }
+    const int off = carry + block_scan(all, warp_sums);
+    carry += warp_sums[32];
+    if (e < E) {
+      before[e] = off + s;                           // part 0's place: only this thread reads it
+      if (b == B) {
+        counts[e] = all;
+        offsets[e] = off;
+        part_loss += all * q;
+      }
+    }
+  }
+  if (b == B) {
+    int live = 0;
+    for (int o = threadIdx.x; o < B; o += blockDim.x) live += hist[static_cast<size_t>(o) * (E + 1) + E];
+    block_scan(live, warp_sums);
+    const double n = warp_sums[32];
+    const double all = block_sum(part_loss, sums);
+    if (threadIdx.x == 0) {
+      counts[E] = static_cast<int32_t>(n);
+      offsets[E] = carry;
+      if (loss != nullptr) *loss = n > 0.0 ? static_cast<float>(all * E / (static_cast<double>(k) * n * n)) : 0.0f;
+    }
+    return;
+  }
+  __syncthreads();
+  const long long first = b * chunk, last = first + chunk < T ? first + chunk : T;
+  route_place(before, ids, pos, row_token, first, last, k);
+}
+
+__device__ __forceinline__ uint32_t pack16(float a, float b, int dtype) {
+  if (dtype == SQ_F16) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+template <int LPT, int EPL>
+__global__ void __launch_bounds__(256)
+route_backward_kernel(const RouteArgs a, const int32_t* __restrict__ ids, const float* __restrict__ gates,
+                      const int32_t* __restrict__ counts, const float* __restrict__ dgates, const float* __restrict__ dloss,
+                      void* dlogits, long long ld_d, int vec_d) {
+  griddep_launch_dependents();
+  griddep_wait();
+  const int sub = threadIdx.x % LPT, E = a.E, k = a.k;
+  const long long groups = static_cast<long long>(gridDim.x) * (blockDim.x / LPT);
+  const long long g0 = blockIdx.x * static_cast<long long>(blockDim.x / LPT) + threadIdx.x / LPT;
+  float c[EPL];
+  {
+    const double n = counts[E];
+    const double w = dloss != nullptr && n > 0.0 ? static_cast<double>(*dloss) * E / (k * n * n) : 0.0;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) c[i] = sub * EPL + i < E ? static_cast<float>(w * counts[sub * EPL + i]) : 0.0f;
+  }
+  const long long rounds = (a.T + groups - 1) / groups;
+  for (long long r = 0; r < rounds; ++r) {           // every group of a warp: the shuffles are the warp's
+    const long long t = g0 + r * groups;
+    const bool in = t < a.T;
+    float x[EPL], p[EPL], d[EPL], m, inv;
+    const bool live = in && (a.mask == nullptr || a.mask[t] != 0);
+    if (live) {
+      route_load<LPT, EPL>(a, t, sub, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) x[i] = RT_NINF;
+    }
+    int id = -1;
+    float dg = 0.0f, g = 0.0f;
+    if (in && sub < k) {
+      id = ids[t * k + sub];
+      if (id >= 0) {
+        dg = dgates != nullptr ? dgates[t * k + sub] : 0.0f;
+        g = gates[t * k + sub];
+      }
+    }
+    route_softmax<LPT, EPL>(x, p, m, inv);
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) d[i] = c[i];
+    float add = dg;
+    if (a.renorm) add = g * (dg - group_sum<LPT>(g * dg));
+    float extra[EPL];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) extra[i] = 0.0f;
+    for (int j = 0; j < k; ++j) {
+      const int e = __shfl_sync(0xFFFFFFFFu, id, j, LPT) - sub * EPL;
+      const float v = __shfl_sync(0xFFFFFFFFu, add, j, LPT);
+#pragma unroll
+      for (int i = 0; i < EPL; ++i)
+        if (e == i) extra[i] += v;
+    }
+    if (!a.renorm) {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) { d[i] += extra[i]; extra[i] = 0.0f; }
+    }
+    float dot = 0.0f;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) dot += p[i] * d[i];
+    dot = group_sum<LPT>(dot);
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) d[i] = p[i] * (d[i] - dot) + extra[i];
+    if (!in) continue;
+    const int e0 = sub * EPL;
+    if (a.dtype == SQ_F32) {
+      float* row = static_cast<float*>(dlogits) + t * ld_d + e0;
+      if (EPL % 4 == 0 && vec_d) {
+        if (e0 < E) {
+#pragma unroll
+          for (int i = 0; i < EPL / 4; ++i)
+            *reinterpret_cast<float4*>(row + 4 * i) = make_float4(d[4 * i], d[4 * i + 1 < EPL ? 4 * i + 1 : 0], d[4 * i + 2 < EPL ? 4 * i + 2 : 0],
+                                                                  d[4 * i + 3 < EPL ? 4 * i + 3 : 0]);
+        }
+      } else if (EPL == 2 && vec_d) {
+        if (e0 < E) *reinterpret_cast<float2*>(row) = make_float2(d[0], d[EPL - 1]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < EPL; ++i)
+          if (e0 + i < E) row[i] = d[i];
+      }
+    } else {
+      unsigned short* row = static_cast<unsigned short*>(dlogits) + t * ld_d + e0;
+      if (EPL % 2 == 0 && vec_d) {
+        if (e0 < E) {
+#pragma unroll
+          for (int i = 0; i < EPL / 2; ++i)
+            *reinterpret_cast<uint32_t*>(row + 2 * i) = pack16(d[2 * i], d[2 * i + 1 < EPL ? 2 * i + 1 : 0], a.dtype);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < EPL; ++i)
+          if (e0 + i < E) row[i] = static_cast<unsigned short>(pack16(d[i], 0.0f, a.dtype) & 0xFFFFu);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Combination
+// ---------------------------------------------------------------------------------------------
+// VEC: eight channels a thread (N % 8 == 0), else one.  Four rows are requested before the first is used.
+template <bool VEC>
+__global__ void __launch_bounds__(256)
+combine_kernel(const __half* __restrict__ Y, long long M, const int32_t* __restrict__ pos, const float* __restrict__ gates,
+               long long T, int k, long long N, __half* __restrict__ out) {
+  griddep_launch_dependents();
+  griddep_wait();
+  constexpr int W = VEC ? 8 : 1;
+  const long long nc = N / W, total = T * nc;
+  for (long long i = blockIdx.x * static_cast<long long>(blockDim.x) + threadIdx.x; i < total;
+       i += static_cast<long long>(gridDim.x) * blockDim.x) {
+    const long long t = i / nc, c = (i - t * nc) * W;
+    float acc[W];
+#pragma unroll
+    for (int w = 0; w < W; ++w) acc[w] = 0.0f;
+    for (int j0 = 0; j0 < k; j0 += 4) {
+      float g[4];
+      uint4 v[4];
+      __half h[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        g[j] = 0.0f;
+        v[j] = make_uint4(0u, 0u, 0u, 0u);
+        h[j] = __ushort_as_half(0);
+        if (j0 + j < k) {
+          const int r = pos[t * k + j0 + j];
+          if (r >= 0 && r < M) {
+            g[j] = gates[t * k + j0 + j];
+            if (VEC) v[j] = __ldg(reinterpret_cast<const uint4*>(Y + static_cast<size_t>(r) * N + c));
+            else h[j] = Y[static_cast<size_t>(r) * N + c];
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (VEC) {
+          const uint32_t u[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[w]));
+            acc[2 * w] = fmaf(g[j], f.x, acc[2 * w]);
+            acc[2 * w + 1] = fmaf(g[j], f.y, acc[2 * w + 1]);
+          }
+        } else {
+          acc[0] = fmaf(g[j], __half2float(h[j]), acc[0]);
+        }
+      }
+    }
+    if constexpr (VEC) {
+      uint4 o;
+      uint32_t* ow = reinterpret_cast<uint32_t*>(&o);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) ow[w] = pack16(acc[2 * w], acc[2 * w + 1], SQ_F16);
+      *reinterpret_cast<uint4*>(out + t * N + c) = o;
+    } else {
+      out[t * N + c] = __float2half_rn(acc[0]);
+    }
+  }
+}
+
+// A block takes a token: its dout is read once for up to four of its rows at a time, whose products with it are added up over
+// the block in a fixed order.
+template <bool VEC>
+__global__ void __launch_bounds__(256)
+combine_backward_kernel(const __half* __restrict__ dout, const __half* __restrict__ Y, long long M, const int32_t* __restrict__ pos,
+                        const float* __restrict__ gates, long long T, int k, long long N, __half* __restrict__ dY,
+                        float* __restrict__ dgates) {
+  griddep_launch_dependents();
+  griddep_wait();
+  constexpr int W = VEC ? 8 : 1;
+  __shared__ float part[4][8];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (long long t = blockIdx.x; t < T; t += gridDim.x) {
+    for (int j0 = 0; j0 < k; j0 += 4) {
+      int r[4];
+      float g[4], s[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        r[j] = j0 + j < k ? pos[t * k + j0 + j] : -1;
+        if (r[j] >= M) r[j] = -1;
+        g[j] = r[j] >= 0 ? gates[t * k + j0 + j] : 0.0f;
+        s[j] = 0.0f;
+      }
+      for (long long c = threadIdx.x * W; c < N; c += 256 * W) {
+        if constexpr (VEC) {
+          const uint4 dv = __ldg(reinterpret_cast<const uint4*>(dout + t * N + c));
+          uint4 yv[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            yv[j] = r[j] >= 0 && dgates != nullptr ? __ldg(reinterpret_cast<const uint4*>(Y + static_cast<size_t>(r[j]) * N + c))
+                                                   : make_uint4(0u, 0u, 0u, 0u);
+          float d[8];
+          const uint32_t du[4] = {dv.x, dv.y, dv.z, dv.w};
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&du[w]));
+            d[2 * w] = f.x;
+            d[2 * w + 1] = f.y;
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (r[j] < 0) continue;
+            const uint32_t yu[4] = {yv[j].x, yv[j].y, yv[j].z, yv[j].w};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&yu[w]));
+              s[j] = fmaf(d[2 * w], f.x, s[j]);
+              s[j] = fmaf(d[2 * w + 1], f.y, s[j]);
+            }
+            if (dY != nullptr) {
+              uint4 o;
+              uint32_t* ow = reinterpret_cast<uint32_t*>(&o);
+#pragma unroll
+              for (int w = 0; w < 4; ++w) ow[w] = pack16(g[j] * d[2 * w], g[j] * d[2 * w + 1], SQ_F16);
+              *reinterpret_cast<uint4*>(dY + static_cast<size_t>(r[j]) * N + c) = o;
+            }
+          }
+        } else {
+          const float d = __half2float(dout[t * N + c]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (r[j] < 0) continue;
+            const size_t o = static_cast<size_t>(r[j]) * N + c;
+            if (dgates != nullptr) s[j] = fmaf(d, __half2float(Y[o]), s[j]);
+            if (dY != nullptr) dY[o] = __float2half_rn(g[j] * d);
+          }
+        }
+      }
+      if (dgates != nullptr) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float v = group_sum<32>(s[j]);
+          if (lane == 0) part[j][warp] = v;
+        }
+        __syncthreads();
+        if (threadIdx.x < 4 && j0 + static_cast<int>(threadIdx.x) < k) {
+          float v = 0.0f;
+#pragma unroll
+          for (int w = 0; w < 8; ++w) v += part[threadIdx.x][w];
+          dgates[t * k + j0 + threadIdx.x] = v;
+        }
+        __syncthreads();
+      }
+    }
+  }
+}
+
+int route_lanes(int E) { return E <= 8 ? 8 : (E <= 16 ? 16 : 32); }
+
+// Blocks of the first kernel: one while a group of lanes has no more than four tokens (the second launch costs more than what
+// more SMs would save), else as many as give every group one.
+int route_blocks(long long T, int E) {
+  const long long groups = RT_THREADS / route_lanes(E);
+  if (T <= 4 * groups) return 1;
+  return static_cast<int>(std::min<long long>(RT_MAX_BLOCKS, (T + groups - 1) / groups));
+}
+
+size_t elem_bytes(int dtype) { return dtype == SQ_F32 ? 4 : 2; }
+
+// Whether a lane's EPL experts may be read or written as one or more whole pieces of up to 16 bytes.
+int route_vec(const void* p, int dtype, int E, long long ld, int epl) {
+  const size_t piece = std::min<size_t>(16, epl * elem_bytes(dtype));
+  return E % epl == 0 && (ld * elem_bytes(dtype)) % piece == 0 && reinterpret_cast<uintptr_t>(p) % piece == 0;
+}
+
+template <typename F>
+sq_status_t with_shape(int E, F f) {
+  if (E <= 8) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 1>());
+  if (E <= 16) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
+  if (E <= 32) return f(std::integral_constant<int, 32>(), std::integral_constant<int, 1>());
+  if (E <= 64) return f(std::integral_constant<int, 32>(), std::integral_constant<int, 2>());
+  if (E <= 128) return f(std::integral_constant<int, 32>(), std::integral_constant<int, 4>());
+  if (E <= 256) return f(std::integral_constant<int, 32>(), std::integral_constant<int, 8>());
+  if (E <= 512) return f(std::integral_constant<int, 32>(), std::integral_constant<int, 16>());
+  return f(std::integral_constant<int, 32>(), std::integral_constant<int, 32>());
+}
+
+}  // namespace
+
+size_t route_workspace_bytes(int64_t T, int32_t E) {
+  const size_t B = route_blocks(T, E);
+  if (B == 1) return 0;
+  return (B * (E + 1) * 4 + 255) / 256 * 256 + (B * E * 4 + 255) / 256 * 256;
+}
+
+sq_status_t launch_route(const void* logits, int dtype, int64_t T, int E, int64_t ld, int k, bool renorm, const void* mask, void* ids,
+                         void* gates, void* counts, void* offsets, void* row_token, void* pos, void* loss, void* workspace,
+                         cudaStream_t s) {
+  const int B = route_blocks(T, E);
+  const long long chunk = (T + B - 1) / B;
+  int32_t* hist = static_cast<int32_t*>(workspace);
+  float* psum = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + (static_cast<size_t>(B) * (E + 1) * 4 + 255) / 256 * 256);
+  int32_t *idsp = static_cast<int32_t*>(ids), *posp = static_cast<int32_t*>(pos), *cnt = static_cast<int32_t*>(counts),
+          *off = static_cast<int32_t*>(offsets), *rt = static_cast<int32_t*>(row_token);
+  const sq_status_t st = with_shape(E, [&](auto lpt, auto epl) -> sq_status_t {
+    constexpr int LPT = decltype(lpt)::value, EPL = decltype(epl)::value;
+    const RouteArgs a = {logits, dtype, E, k, T, ld, renorm ? 1 : 0, route_vec(logits, dtype, E, ld, EPL), static_cast<const uint8_t*>(mask)};
+    auto kern = route_kernel<LPT, EPL>;
+    const int smem = (2 * (RT_THREADS / LPT) + 1) * E * 4;
+    if (!ensure_dyn_smem(reinterpret_cast<const void*>(kern), smem)) return SQ_ERR_CUDA;
+    const cudaError_t err = launch_maybe_pdl(kern, dim3(static_cast<unsigned>(B)), dim3(RT_THREADS), static_cast<size_t>(smem), s, a, chunk,
+                                             idsp, static_cast<float*>(gates), posp, hist, psum, cnt, off, rt, static_cast<float*>(loss));
+    count_launch();
+    return err == cudaSuccess ? SQ_OK : SQ_ERR_CUDA;
+  });
+  if (st != SQ_OK || B == 1) return st;
+  const int smem = 3 * std::max(1, 1024 / E) * E * 4;
+  const cudaError_t err = launch_dependent(route_finish_kernel, dim3(static_cast<unsigned>(B + 1)), dim3(1024), static_cast<size_t>(smem), s, B,
+                                           E, k, static_cast<long long>(T), chunk, static_cast<const int32_t*>(hist),
+                                           static_cast<const float*>(psum), static_cast<const int32_t*>(idsp), posp, cnt, off, rt,
+                                           static_cast<float*>(loss));
+  count_launch();
+  return err == cudaSuccess ? SQ_OK : SQ_ERR_CUDA;
+}
+
+sq_status_t launch_route_backward(const void* logits, int dtype, int64_t T, int E, int64_t ld, int k, bool renorm, const void* mask,
+                                  const void* ids, const void* gates, const void* counts, const void* dgates, const void* dloss,
+                                  void* dlogits, int64_t ld_d, cudaStream_t s) {
+  const int sms = sm_count();
+  if (sms <= 0) return SQ_ERR_CUDA;
+  return with_shape(E, [&](auto lpt, auto epl) -> sq_status_t {
+    constexpr int LPT = decltype(lpt)::value, EPL = decltype(epl)::value;
+    const RouteArgs a = {logits, dtype, E, k, T, ld, renorm ? 1 : 0, route_vec(logits, dtype, E, ld, EPL), static_cast<const uint8_t*>(mask)};
+    const long long blocks = (T + 256 / LPT - 1) / (256 / LPT);
+    const unsigned grid = static_cast<unsigned>(std::min<long long>(blocks, static_cast<long long>(sms) * 8));
+    const cudaError_t err = launch_maybe_pdl(route_backward_kernel<LPT, EPL>, dim3(grid), dim3(256), 0, s, a, static_cast<const int32_t*>(ids),
+                                             static_cast<const float*>(gates), static_cast<const int32_t*>(counts),
+                                             static_cast<const float*>(dgates), static_cast<const float*>(dloss), dlogits,
+                                             static_cast<long long>(ld_d), route_vec(dlogits, dtype, E, ld_d, EPL));
+    count_launch();
+    return err == cudaSuccess ? SQ_OK : SQ_ERR_CUDA;
+  });
+}
+
+sq_status_t launch_combine(const void* Y, int64_t M, const void* pos, const void* gates, int64_t T, int k, int64_t N, void* out,
+                           cudaStream_t s) {
+  const int sms = sm_count();
+  if (sms <= 0) return SQ_ERR_CUDA;
+  const bool vec = N % 8 == 0;
+  const long long work = T * (vec ? N / 8 : N);
+  const unsigned grid = static_cast<unsigned>(std::min<long long>((work + 255) / 256, static_cast<long long>(sms) * 8));
+  const cudaError_t err = launch_maybe_pdl(vec ? combine_kernel<true> : combine_kernel<false>, dim3(grid), dim3(256), 0, s,
+                                           static_cast<const __half*>(Y), static_cast<long long>(M), static_cast<const int32_t*>(pos),
+                                           static_cast<const float*>(gates), static_cast<long long>(T), k, static_cast<long long>(N),
+                                           static_cast<__half*>(out));
+  count_launch();
+  return err == cudaSuccess ? SQ_OK : SQ_ERR_CUDA;
+}
+
+sq_status_t launch_combine_backward(const void* dout, const void* Y, int64_t M, const void* pos, const void* gates, int64_t T, int k,
+                                    int64_t N, void* dY, void* dgates, cudaStream_t s) {
+  const int sms = sm_count();
+  if (sms <= 0) return SQ_ERR_CUDA;
+  const unsigned grid = static_cast<unsigned>(std::min<long long>(T, static_cast<long long>(sms) * 8));
+  const cudaError_t err = launch_maybe_pdl(N % 8 == 0 ? combine_backward_kernel<true> : combine_backward_kernel<false>, dim3(grid), dim3(256),
+                                           0, s, static_cast<const __half*>(dout), static_cast<const __half*>(Y), static_cast<long long>(M),
+                                           static_cast<const int32_t*>(pos), static_cast<const float*>(gates), static_cast<long long>(T), k,
+                                           static_cast<long long>(N), static_cast<__half*>(dY), static_cast<float*>(dgates));
+  count_launch();
+  return err == cudaSuccess ? SQ_OK : SQ_ERR_CUDA;
+}
+
+}  // namespace sq
