@@ -6,6 +6,7 @@
 #include <algorithm>
 
 #include "sq_internal.h"
+#include "sq_groups.cuh"
 #include "sq_ptx.cuh"
 
 namespace sq {
@@ -100,56 +101,6 @@ __device__ __forceinline__ uint4 lds128_at(uint32_t a) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
   return v;
-}
-
-// code * scale (+ offset) of a word's eight weights, pairs as widen_word leaves them.
-template <bool BIAS>
-__device__ __forceinline__ uint4 scaled_word(uint32_t word, const WidenConsts& k, __half2 s, __half2 b) {
-  const uint4 c = widen_word(word, k);
-  auto f = [&](uint32_t x) {
-    const __half2 h = *reinterpret_cast<const __half2*>(&x);
-    const __half2 r = BIAS ? __hfma2(h, s, b) : __hmul2(h, s);
-    return *reinterpret_cast<const uint32_t*>(&r);
-  };
-  return make_uint4(f(c.x), f(c.y), f(c.z), f(c.w));
-}
-
-// Rows [lo, hi) of expert e, within [0, M).
-__device__ __forceinline__ void expert_rows(const GsArgs& a, int e, long long& lo, long long& hi) {
-  const long long M = a.M, b = a.offsets[e], d = a.offsets[e + 1];
-  lo = b < 0 ? 0 : (b < M ? b : M);
-  hi = d < lo ? lo : (d < M ? d : M);
-}
-
-// The experts' rows cut into chunks of `rows` each: first[e] = chunks of the experts before e, first[E] = all.  All threads.
-__device__ __forceinline__ void expert_chunks(const GsArgs& a, int rows, int* first) {
-  __shared__ int sums[33];
-  int carry = 0;
-  for (int e0 = 0; e0 < a.E; e0 += static_cast<int>(blockDim.x)) {
-    const int e = e0 + static_cast<int>(threadIdx.x);
-    int c = 0;
-    if (e < a.E) {
-      long long lo, hi;
-      expert_rows(a, e, lo, hi);
-      c = static_cast<int>((hi - lo + rows - 1) / rows);
-    }
-    const int off = carry + block_scan(c, sums);
-    if (e < a.E) first[e] = off;
-    carry += sums[32];
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) first[a.E] = carry;
-  __syncthreads();
-}
-// The expert of a chunk: the last e with first[e] <= chunk (an expert without chunks has the same first as the next).
-__device__ __forceinline__ int chunk_expert(const int* first, int E, int chunk) {
-  int lo = 0, hi = E;
-  while (lo + 1 < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (first[mid] <= chunk) lo = mid;
-    else hi = mid;
-  }
-  return lo;
 }
 
 template <int RB, int NT, bool BIAS, bool EXPERTS>
@@ -360,6 +311,20 @@ gs_stream_kernel(const __grid_constant__ GsArgs a, int R, int splits) {
   cp_async_wait<0>();
 }
 
+// out[r] = Z[row_token[r]], zeros for a token that does not exist; rows of no expert are not needed.
+__global__ void __launch_bounds__(256)
+gs_gather_kernel(const __grid_constant__ GsArgs a, uint4* __restrict__ out) {
+  griddep_launch_dependents();
+  griddep_wait();
+  const int per_row = a.K / 8;
+  const long long rows = max(0ll, min(static_cast<long long>(a.offsets[a.E]), static_cast<long long>(a.M)));
+  const uint4* Z = reinterpret_cast<const uint4*>(a.Z);
+  for (long long i = blockIdx.x * 256ll + threadIdx.x; i < rows * per_row; i += gridDim.x * 256ll) {
+    const long long r = i / per_row, tok = a.row_token[r];
+    out[i] = tok >= 0 && tok < a.T ? __ldg(Z + tok * per_row + (i - r * per_row)) : make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+
 // Rows of fp16 or fp32 values -> codes in the weight-only order, scales and offsets per group.  A thread takes a word of eight
 // channels, group / 8 neighbouring lanes a group; rows are padded to whole groups, so that every lane of a group is here.
 template <typename V>
@@ -493,12 +458,47 @@ sq_status_t launch_stream(const GsArgs& a, cudaStream_t s) {
   return launch_stream_any<false>(a, nt, best_r, best_s, best_grid, s);
 }
 
+// Rows of a token tile of the CTA-pair kernel for experts (a multiple of 32 up to 256), as for a dense product: waves of tiles,
+// each of a time of about width + 70, with every expert's last tile half full.
+int gs_tile_m(const GsArgs& a) {
+  const int pairs = std::max(1, sm_count() / 2);
+  const double ch_tiles = static_cast<double>((a.N + 255) / 256), experts = static_cast<double>(std::min<int64_t>(a.E, a.M));
+  int best = 256;
+  double best_cost = 0.0;
+  for (int w = 256; w >= 32; w -= 32) {
+    const double load = ch_tiles * (experts * (a.M / experts / w + 0.5)) / pairs;
+    const double cost = std::max(1.0, load) * (w + 70);
+    if (w == 256 || cost < best_cost) {
+      best = w;
+      best_cost = cost;
+    }
+  }
+  return best;
+}
+
 }  // namespace
 
 sq_status_t launch_gemm_gs(const GsArgs& a, void* workspace, cudaStream_t s) {
-  (void)workspace;
-  const bool stream = a.K % 32 == 0 && a.N % 2 == 0 && (a.E > 0 ? a.M <= 16 * static_cast<int64_t>(a.E) : a.M <= 16);
-  if (stream) return launch_stream(a, s);
+  const bool few = a.E > 0 ? a.M <= 16 * static_cast<int64_t>(a.E) : a.M <= 16;
+  if (a.K % 32 == 0 && a.N % 2 == 0 && few) return launch_stream(a, s);
+  // (32-bit coordinates of a tile in the weights and in the rows)
+  const int64_t kMax = (1ll << 31) - 1024;
+  if (a.K % 32 == 0 && a.M <= kMax && a.N * std::max(a.E, 1) <= kMax) {
+    if (a.E == 0) return launch_wo_gemm_groups(a, 0, s);
+    GsArgs b = a;
+    if (a.row_token) {
+      // The rows in their order, so that a tile of them is one TMA box.
+      const int64_t pieces = a.M * (a.K / 8);
+      const unsigned grid = static_cast<unsigned>(std::min<int64_t>((pieces + 255) / 256, static_cast<int64_t>(std::max(sm_count(), 1)) * 8));
+      const cudaError_t err = launch_maybe_pdl(gs_gather_kernel, dim3(grid), dim3(256), 0, s, a, static_cast<uint4*>(workspace));
+      count_launch();
+      if (err != cudaSuccess) return SQ_ERR_CUDA;
+      b.Z = static_cast<const __half*>(workspace);
+      b.row_token = nullptr;
+      b.T = a.M;
+    }
+    return launch_wo_gemm_groups(b, gs_tile_m(a), s);
+  }
   const dim3 grid(static_cast<unsigned>((a.N + 127) / 128), static_cast<unsigned>(std::min<long long>(a.M, 65535)));
   const cudaError_t err = launch_maybe_pdl(gs_simple_kernel, grid, dim3(128), 0, s, a);
   count_launch();

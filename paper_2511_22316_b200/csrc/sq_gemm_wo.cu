@@ -23,6 +23,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "sq_groups.cuh"
 #include "sq_internal.h"
 #include "sq_ptx.cuh"
 
@@ -84,6 +85,71 @@ __device__ __forceinline__ uint4 widen_word(uint32_t word, const WidenConsts& k)
   const uint32_t w8 = word >> 8;
   return make_uint4(widen_low(word, k), widen_high(word, k), widen_low(w8, k), widen_high(w8, k));
 }
+
+// code * scale (+ offset) of a word's eight weights, pairs as widen_word leaves them.
+template <bool BIAS>
+__device__ __forceinline__ uint4 scaled_word(uint32_t word, const WidenConsts& k, __half2 s, __half2 b) {
+  const uint4 c = widen_word(word, k);
+  auto f = [&](uint32_t x) {
+    const __half2 h = *reinterpret_cast<const __half2*>(&x);
+    const __half2 r = BIAS ? __hfma2(h, s, b) : __hmul2(h, s);
+    return *reinterpret_cast<const uint32_t*>(&r);
+  };
+  return make_uint4(f(c.x), f(c.y), f(c.z), f(c.w));
+}
+
+// What the two kernels with the weights in tensor memory multiply with: codes, and a step per channel behind the sums; or weights
+// with group scales (sq_gemm_gs.cu), scaled while they are widened, dense or over experts whose rows the router sorted.
+struct WoPlain {
+  static constexpr bool GS = false, BIAS = false, EXPERTS = false;
+};
+template <bool BIAS_, bool EXPERTS_>
+struct WoGroups {
+  static constexpr bool GS = true, BIAS = BIAS_, EXPERTS = EXPERTS_;
+  GsArgs a;
+};
+
+// A tile's place: its first channel, that channel's row among all weights, its rows of the tokens, and its expert.
+struct WoTile {
+  int ch0, wrow0, tok0, tok_end, expert;
+};
+template <class X>
+__device__ __forceinline__ WoTile wo_tile(const X& x, const int* first, int tile, int tiles_n, int width_n, int width_m, int M, int N) {
+  WoTile p;
+  const int chunk = tile / tiles_n;
+  p.ch0 = (tile - chunk * tiles_n) * width_n;
+  p.wrow0 = p.ch0;
+  p.tok0 = chunk * width_m;
+  p.tok_end = M;
+  p.expert = 0;
+  if constexpr (X::EXPERTS) {
+    p.expert = chunk_expert(first, x.a.E, chunk);
+    long long lo, hi;
+    expert_rows(x.a, p.expert, lo, hi);
+    p.wrow0 += p.expert * N;
+    p.tok0 = static_cast<int>(lo) + (chunk - first[p.expert]) * width_m;
+    p.tok_end = static_cast<int>(hi);
+  }
+  return p;
+}
+
+// The scales (and offsets) of one channel for the eight pieces of 32 input channels of a stage.
+template <class X>
+struct WoScales {
+  __half s[8], b[8];
+  __device__ __forceinline__ void load(const X& x, int expert, int ch, int sb) {
+    const GsArgs& a = x.a;
+    const size_t N = static_cast<size_t>(a.N), G = (a.K + a.group - 1) / a.group;
+    const size_t at = static_cast<size_t>(expert) * G * N + min(ch, static_cast<int>(a.N) - 1);
+    const int shift = 31 - __clz(a.group);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const size_t o = at + static_cast<size_t>(min(sb * 256 + i * 32, a.K - 1) >> shift) * N;
+      s[i] = __ldg(a.sg + o);
+      if (X::BIAS) b[i] = __ldg(a.bg + o);
+    }
+  }
+};
 
 // Widens k-block h (64 channels = 32 packed bytes) of BN staged rows into BN x 64 fp16.  Staging and
 // operand rows are 128 bytes with the 128-byte swizzle (16-byte chunk c of row r sits at chunk
@@ -343,10 +409,11 @@ struct WoDecSmem {
   static constexpr int DYN_BYTES = TOTAL + 1024;
 };
 
-template <int NT, int ST, int SS, int CT>
+template <int NT, int ST, int SS, int CT, class X>
 __global__ void __launch_bounds__(WOD_THREADS, 1)
 wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_constant__ CUtensorMap tmap_w,
-                      const __half* __restrict__ sw, int M, int N, int K, __half* __restrict__ Y, int splits) {
+                      const __half* __restrict__ sw, int M, int N, int K, __half* __restrict__ Y, int splits,
+                      const __grid_constant__ X x) {
   using L = WoDecSmem<NT, ST, SS>;
   // CT = channel tiles of 128 that share a token tile (1 or 2).  With one, two accumulators alternate
   // between tiles (the epilogue of a tile runs under the next tile's MMAs); with two, both accumulators
@@ -372,7 +439,8 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_TMEM);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int num_kb = K / 64;
+  static_assert(!X::EXPERTS && (!X::GS || CT == 1), "group scales: one channel tile, dense");
+  const int num_kb = X::GS ? (K + 63) / 64 : K / 64;      // (with group scales K % 32 == 0 will do: the rest of a block is zeros)
   const int num_sb = (num_kb + 3) / 4;        // stages per tile (the last may hold fewer than four k-blocks)
   // A tile is 128 channels x NT tokens; the channel tiles run fastest, so that the CTAs at work at one
   // time share a few token tiles (which stay in L2) and stream different weights.
@@ -520,6 +588,25 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
     const int grp = (warp - 2) >> 2;                    // this group's stages: it % WOD_CONV_GROUPS == grp
     const int r = q * 32 + lane;                        // channel of the tile = TMEM lane
     const uint32_t lane_addr = static_cast<uint32_t>(q * 32) << 16;
+    // Scales one stage of this group ahead: a cursor of its own walks the same stages.
+    WoScales<X> sc, next;
+    int ntile = cid, nsb = sb0;
+    auto skip = [&](int n) {
+      for (; n > 0; --n)
+        if (++nsb >= sb1) {
+          nsb = sb0;
+          ntile += ncl;
+        }
+    };
+    auto fetch = [&](WoScales<X>& to) {
+      if constexpr (X::GS) {
+        if (ntile >= num_tiles || sb0 >= sb1) return;
+        const WoTile p = wo_tile(x, nullptr, ntile, tiles_n, 128 * CT, NT, M, N);
+        to.load(x, p.expert, p.ch0 + r, nsb);
+      }
+    };
+    skip(grp);
+    fetch(sc);
     uint32_t it = 0;
     bool ok = true;
     for (int tile = cid; tile < num_tiles && ok; tile += ncl) {
@@ -534,6 +621,10 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
         uint4 w[8];
 #pragma unroll
         for (int c = 0; c < 8; ++c) w[c] = *reinterpret_cast<const uint4*>(row + ((c ^ (r & 7)) << 4));
+        if constexpr (X::GS) {
+          skip(WOD_CONV_GROUPS);
+          fetch(next);
+        }
         ok = mbar_wait(&a_empty[sa], ((it / WOD_A_STAGES) & 1) ^ 1, WO_B_EMPTY, limit);
         if (!ok) break;
         tc_fence_after_sync();
@@ -547,7 +638,10 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
               const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
               for (int g = 0; g < 4; ++g) {
-                const uint4 f = widen_word(xs[g], wk);
+                uint4 f;
+                if constexpr (X::GS)
+                  f = scaled_word<X::BIAS>(xs[g], wk, __half2half2(sc.s[2 * h + j]), __half2half2(X::BIAS ? sc.b[2 * h + j] : sc.s[2 * h + j]));
+                else f = widen_word(xs[g], wk);
                 v[16 * j + 4 * g + 0] = f.x;
                 v[16 * j + 4 * g + 1] = f.y;
                 v[16 * j + 4 * g + 2] = f.z;
@@ -564,6 +658,7 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
           mbar_arrive(&a_full[sa]);
           mbar_arrive(&st_empty[ss]);
         }
+        if constexpr (X::GS) sc = next;
       }
     }
   } else {
@@ -578,7 +673,7 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
       const int tok0 = (tile / tiles_n) * NT;
       float swh[CT];
 #pragma unroll
-      for (int half = 0; half < CT; ++half) swh[half] = (ch0 + 128 * half < N) ? __half2float(sw[ch0 + 128 * half]) : 0.0f;
+      for (int half = 0; half < CT; ++half) swh[half] = X::GS ? 1.0f : (ch0 + 128 * half < N) ? __half2float(sw[ch0 + 128 * half]) : 0.0f;
       ok = mbar_wait(&tmem_full[b], (tcount / NBUF) & 1, WO_TMEM_FULL, limit);
       if (!ok) break;
       tc_fence_after_sync();
@@ -636,7 +731,7 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
       const int quarter = warp & 3;
       const int ch = (cid % tiles_n) * 128 + quarter * 32 + lane;                          // CT = 1 here
       const int tok0 = (cid / tiles_n) * NT;
-      const float swv = (ch < N) ? __half2float(sw[ch]) : 0.0f;
+      const float swv = X::GS ? 1.0f : (ch < N) ? __half2float(sw[ch]) : 0.0f;
       const uint32_t tmem_d = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);     // accumulator 0: one tile
       const float* part = reinterpret_cast<const float*>(smem + L::OFF_T);
 #pragma unroll
@@ -717,10 +812,10 @@ struct WoPairSmem {
   static constexpr int DYN_BYTES = TOTAL + 1024;
 };
 
-template <int SS>
+template <int SS, class X>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WP_THREADS, 1)
 wo_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_constant__ CUtensorMap tmap_w,
-                    const __half* __restrict__ sw, int M, int N, int K, int tile_m, __half* __restrict__ Y) {
+                    const __half* __restrict__ sw, int M, int N, int K, int tile_m, __half* __restrict__ Y, const __grid_constant__ X x) {
   using L = WoPairSmem<SS>;
   static_assert(SS % WOD_CONV_GROUPS == 0, "a converter group meets every phase of its stages");
   griddep_launch_dependents();
@@ -739,11 +834,17 @@ wo_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();            // 0 = leader (issues the MMAs)
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
-  const int num_kb = K / 64;
+  const int num_kb = X::GS ? (K + 63) / 64 : K / 64;
   const int num_sb = (num_kb + 3) / 4;                // stages per tile (the last may hold fewer than four k-blocks)
   // channel tiles run fastest: the pairs at work at one time share a few token tiles, which stay in L2
   const int tiles_n = (N + 255) / 256;
-  const int num_tiles = tiles_n * ((M + tile_m - 1) / tile_m);
+  int num_tiles = tiles_n * ((M + tile_m - 1) / tile_m);
+  __shared__ int first[X::EXPERTS ? 1025 : 1];          // the experts' token tiles
+  if constexpr (X::EXPERTS) {
+    griddep_wait();                                     // the offsets come from the router
+    expert_chunks(x.a, tile_m, first);
+    num_tiles = tiles_n * first[x.a.E];
+  }
   const uint32_t limit = wait_limit();
 
   // The weights do not depend on the kernel before this one: the first ring-full of them is requested
@@ -758,7 +859,7 @@ wo_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
       while (pre < SS && t < num_tiles) {
         mbar_arrive_expect_tx(&st_full[pre], L::W_ST);
         tma_load_2d(smem + L::OFF_W_ST + pre * L::W_ST, &tmap_w, &st_full[pre], sb * 128,
-                    (t % tiles_n) * 256 + static_cast<int>(rank) * 128);
+                    wo_tile(x, first, t, tiles_n, 256, tile_m, M, N).wrow0 + static_cast<int>(rank) * 128);
         ++pre;
         if (++sb >= num_sb) {
           sb = 0;
@@ -793,7 +894,7 @@ wo_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
       uint32_t it = 0;
       bool ok = true;
       for (int tile = pair; tile < num_tiles && ok; tile += npairs) {
-        const int ch0 = (tile % tiles_n) * 256 + static_cast<int>(rank) * 128;
+        const int ch0 = wo_tile(x, first, tile, tiles_n, 256, tile_m, M, N).wrow0 + static_cast<int>(rank) * 128;
         for (int sb = 0; sb < num_sb; ++sb, ++it) {
           if (it < static_cast<uint32_t>(pre)) continue;
           const int ss = it % SS;
@@ -811,7 +912,7 @@ wo_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
       uint32_t it = 0;
       bool ok = true;
       for (int tile = pair; tile < num_tiles && ok; tile += npairs) {
-        const int tok0 = (tile / tiles_n) * tile_m + static_cast<int>(rank) * (tile_m / 2);
+        const int tok0 = wo_tile(x, first, tile, tiles_n, 256, tile_m, M, N).tok0 + static_cast<int>(rank) * (tile_m / 2);
         for (int sb = 0; sb < num_sb; ++sb, ++it) {
           const int s = it % WP_S;
           const int nk = (num_kb - 4 * sb) < 4 ? (num_kb - 4 * sb) : 4;
@@ -863,6 +964,25 @@ wo_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
     const int grp = (warp - 2) >> 2;                    // this group's ring stage
     const int r = q * 32 + lane;                        // channel of the CTA's 128 = TMEM lane
     const uint32_t lane_addr = static_cast<uint32_t>(q * 32) << 16;
+    // Scales one stage of this group ahead: a cursor of its own walks the same stages.
+    WoScales<X> sc, next;
+    int ntile = pair, nsb = 0;
+    auto skip = [&](int n) {
+      for (; n > 0; --n)
+        if (++nsb >= num_sb) {
+          nsb = 0;
+          ntile += npairs;
+        }
+    };
+    auto fetch = [&](WoScales<X>& to) {
+      if constexpr (X::GS) {
+        if (ntile >= num_tiles || 0 >= num_sb) return;
+        const WoTile p = wo_tile(x, first, ntile, tiles_n, 256, tile_m, M, N);
+        to.load(x, p.expert, p.ch0 + static_cast<int>(rank) * 128 + r, nsb);
+      }
+    };
+    skip(grp);
+    fetch(sc);
     uint32_t it = 0;
     bool ok = true;
     for (int tile = pair; tile < num_tiles && ok; tile += npairs) {
@@ -876,6 +996,10 @@ wo_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
         uint4 w[8];
 #pragma unroll
         for (int c = 0; c < 8; ++c) w[c] = *reinterpret_cast<const uint4*>(row + ((c ^ (r & 7)) << 4));
+        if constexpr (X::GS) {
+          skip(WOD_CONV_GROUPS);
+          fetch(next);
+        }
         ok = mbar_wait(&empty[s], ((it / WP_S) & 1) ^ 1, WP_EMPTY_A, limit);
         if (!ok) break;
         tc_fence_after_sync();
@@ -889,7 +1013,10 @@ wo_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
               const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
               for (int g = 0; g < 4; ++g) {
-                const uint4 f = widen_word(xs[g], wk);
+                uint4 f;
+                if constexpr (X::GS)
+                  f = scaled_word<X::BIAS>(xs[g], wk, __half2half2(sc.s[2 * h + j]), __half2half2(X::BIAS ? sc.b[2 * h + j] : sc.s[2 * h + j]));
+                else f = widen_word(xs[g], wk);
                 v[16 * j + 4 * g + 0] = f.x;
                 v[16 * j + 4 * g + 1] = f.y;
                 v[16 * j + 4 * g + 2] = f.z;
@@ -909,6 +1036,7 @@ wo_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
           mbar_arrive_cluster(&full[s], 0);
           mbar_arrive(&st_empty[ss]);
         }
+        if constexpr (X::GS) sc = next;
       }
     }
   } else {
@@ -921,9 +1049,10 @@ wo_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
     uint32_t tcount = 0;
     bool ok = true;
     for (int tile = pair; tile < num_tiles && ok; tile += npairs, ++tcount) {
-      const int ch = (tile % tiles_n) * 256 + static_cast<int>(rank) * 128 + q * 32 + lane;
-      const int tok0 = (tile / tiles_n) * tile_m;
-      const float swv = (ch < N) ? __half2float(sw[ch]) : 0.0f;
+      const WoTile place = wo_tile(x, first, tile, tiles_n, 256, tile_m, M, N);
+      const int ch = place.ch0 + static_cast<int>(rank) * 128 + q * 32 + lane;
+      const int tok0 = place.tok0;
+      const float swv = X::GS ? 1.0f : (ch < N) ? __half2float(sw[ch]) : 0.0f;
       ok = mbar_wait(tmem_full, tcount & 1, WP_TMEM_FULL, limit);
       if (!ok) break;
       tc_fence_after_sync();
@@ -942,7 +1071,7 @@ wo_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const int tok = tok0 + c * 16 + e;
-            if (tok < M) Y[static_cast<size_t>(tok) * N + ch] = __float2half_rn(__uint_as_float(r[e]) * swv);
+            if (tok < place.tok_end) Y[static_cast<size_t>(tok) * N + ch] = __float2half_rn(__uint_as_float(r[e]) * swv);
           }
         }
       }
@@ -1143,9 +1272,9 @@ sq_status_t launch_wo_tc(const void* Z16, const void* Wq, const void* sw, int M,
   return (err == cudaSuccess && cudaGetLastError() == cudaSuccess) ? SQ_OK : SQ_ERR_CUDA;
 }
 
-template <int NT, int ST, int SS, int CT = 1>
+template <int NT, int ST, int SS, int CT = 1, class X = WoPlain>
 sq_status_t launch_wo_decode(const void* Z16, const void* Wq, const void* sw, int M, int N, int K, void* Y,
-                             cudaStream_t s) {
+                             cudaStream_t s, const X& x = X()) {
   using L = WoDecSmem<NT, ST, SS>;
   static_assert(L::DYN_BYTES <= 227 * 1024, "shared-memory plan does not fit");
   EncodeTiledFn enc = get_encode_fn();
@@ -1160,20 +1289,20 @@ sq_status_t launch_wo_decode(const void* Z16, const void* Wq, const void* sw, in
           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return SQ_ERR_CUDA;
   if (!make_packed_map(&mw, Wq, N, K / 2, 128)) return SQ_ERR_CUDA;
-  auto kern = wo_gemm_tmem_kernel<NT, ST, SS, CT>;
+  auto kern = wo_gemm_tmem_kernel<NT, ST, SS, CT, X>;
   if (!ensure_dyn_smem(reinterpret_cast<const void*>(kern), L::DYN_BYTES)) return SQ_ERR_CUDA;
   const int sms = sm_count();
   if (sms <= 0) return SQ_ERR_CUDA;
   const int tiles = ((N + 128 * CT - 1) / (128 * CT)) * ((M + NT - 1) / NT);
   // K over clusters of 2 or 4 CTAs where the tiles alone would leave more than half of the SMs idle and
   // every CTA still gets at least four 256-channel stages; each cluster then has exactly one tile.
-  const int num_sb = (K / 64 + 3) / 4;
+  const int num_sb = (K + 255) / 256;
   int splits = 1;
   while (CT == 1 && splits < 4 && tiles * splits * 2 <= sms && num_sb / (splits * 2) >= 4) splits *= 2;
   const int grid = splits > 1 ? tiles * splits : (tiles < sms ? tiles : sms);
   const cudaError_t err = launch_cluster_maybe_pdl(kern, dim3(grid), dim3(WOD_THREADS), L::DYN_BYTES, s,
                                                    static_cast<unsigned>(splits), mz, mw, static_cast<const __half*>(sw),
-                                                   M, N, K, static_cast<__half*>(Y), splits);
+                                                   M, N, K, static_cast<__half*>(Y), splits, x);
   count_launch();
   return (err == cudaSuccess && cudaGetLastError() == cudaSuccess) ? SQ_OK : SQ_ERR_CUDA;
 }
@@ -1202,8 +1331,10 @@ int wo_pair_tile_m(int M, int N, int pairs) {
   return best;
 }
 
-template <int SS>
-sq_status_t launch_wo_pair(const void* Z16, const void* Wq, const void* sw, int M, int N, int K, void* Y, cudaStream_t s) {
+// `weight_rows`: of all experts.  `tile_m`: 0 = by wo_pair_tile_m, which counts the tiles of a dense product.
+template <int SS, class X = WoPlain>
+sq_status_t launch_wo_pair(const void* Z16, const void* Wq, const void* sw, int M, int N, int K, void* Y, cudaStream_t s,
+                           const X& x = X(), int weight_rows = 0, int tile_m = 0) {
   using L = WoPairSmem<SS>;
   static_assert(L::DYN_BYTES <= 227 * 1024, "shared-memory plan does not fit");
   EncodeTiledFn enc = get_encode_fn();
@@ -1213,20 +1344,20 @@ sq_status_t launch_wo_pair(const void* Z16, const void* Wq, const void* sw, int 
   const cuuint64_t strides[1] = {static_cast<cuuint64_t>(K) * 2};
   const int sms = sm_count();
   if (sms <= 0) return SQ_ERR_CUDA;
-  const int tile_m = wo_pair_tile_m(M, N, sms / 2);
+  if (tile_m == 0) tile_m = wo_pair_tile_m(M, N, sms / 2);
   const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(tile_m / 2)};
   const cuuint32_t estr[2] = {1, 1};
   if (enc(&mz, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(Z16), dims, strides, box, estr,
           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return SQ_ERR_CUDA;
-  if (!make_packed_map(&mw, Wq, N, K / 2, 128)) return SQ_ERR_CUDA;
-  auto kern = wo_gemm_pair_kernel<SS>;
+  if (!make_packed_map(&mw, Wq, X::EXPERTS ? weight_rows : N, K / 2, 128)) return SQ_ERR_CUDA;
+  auto kern = wo_gemm_pair_kernel<SS, X>;
   if (!ensure_dyn_smem(reinterpret_cast<const void*>(kern), L::DYN_BYTES)) return SQ_ERR_CUDA;
-  const int tiles = ((N + 255) / 256) * ((M + tile_m - 1) / tile_m);
-  const int pairs = tiles < sms / 2 ? tiles : sms / 2;
+  const int64_t tiles = ((N + 255ll) / 256) * ((M + tile_m - 1) / tile_m + (X::EXPERTS ? weight_rows / N : 0));
+  const int pairs = static_cast<int>(std::min<int64_t>(tiles, sms / 2));
   const cudaError_t err = launch_maybe_pdl(kern, dim3(2 * pairs), dim3(WP_THREADS), L::DYN_BYTES, s, mz, mw,
-                                           static_cast<const __half*>(sw), M, N, K, tile_m, static_cast<__half*>(Y));
+                                           static_cast<const __half*>(sw), M, N, K, tile_m, static_cast<__half*>(Y), x);
   count_launch();
   return (err == cudaSuccess && cudaGetLastError() == cudaSuccess) ? SQ_OK : SQ_ERR_CUDA;
 }
@@ -1295,6 +1426,25 @@ sq_status_t launch_wo_gemm(const void* Z16, const void* Wq, const void* sw, int6
                                                static_cast<__half*>(Y));
   count_launch();
   return cudaGetLastError() == cudaSuccess ? SQ_OK : SQ_ERR_CUDA;
+}
+
+sq_status_t launch_wo_gemm_groups(const GsArgs& a, int tile_m, cudaStream_t s) {
+  const int M = static_cast<int>(a.M), N = static_cast<int>(a.N);
+  if (a.E > 0) {
+    const int rows = static_cast<int>(a.E * a.N);
+    if (a.bg) return launch_wo_pair<4, WoGroups<true, true>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a}, rows, tile_m);
+    return launch_wo_pair<4, WoGroups<false, true>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a}, rows, tile_m);
+  }
+  if (M <= 32) {
+    if (a.bg) return launch_wo_decode<32, 4, 8, 1, WoGroups<true, false>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
+    return launch_wo_decode<32, 4, 8, 1, WoGroups<false, false>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
+  }
+  if (M <= 64) {
+    if (a.bg) return launch_wo_decode<64, 3, 6, 1, WoGroups<true, false>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
+    return launch_wo_decode<64, 3, 6, 1, WoGroups<false, false>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
+  }
+  if (a.bg) return launch_wo_pair<4, WoGroups<true, false>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a}, 0, tile_m);
+  return launch_wo_pair<4, WoGroups<false, false>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a}, 0, tile_m);
 }
 
 sq_status_t launch_interleave_nibbles(void* Wq, int64_t rows, int64_t K, cudaStream_t s) {

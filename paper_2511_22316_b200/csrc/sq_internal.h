@@ -220,6 +220,9 @@ struct GsArgs {
   int K, group, E;                 // E = 0: dense
 };
 sq_status_t launch_gemm_gs(const GsArgs& a, void* workspace, cudaStream_t s);
+// The tensor-memory kernels of the weight-only product with group scales (sq_gemm_wo.cu): K % 32 == 0; experts by CTA pairs, their
+// rows in order (no row_token), tiles of tile_m rows; dense with tile_m = 0.
+sq_status_t launch_wo_gemm_groups(const GsArgs& a, int tile_m, cudaStream_t s);
 // `rows` rows of X (fp16 or fp32, [rows x K]) are rows row0 .. of a weight matrix of N channels.
 sq_status_t launch_quant_groups(const void* X, bool f32, int64_t rows, int64_t row0, int64_t N, int K, int group, int bits, void* Wq,
                                 void* sg, void* bg, cudaStream_t s);

@@ -20,6 +20,7 @@
 #include <type_traits>
 
 #include "sq_internal.h"
+#include "sq_groups.cuh"
 #include "sq_ptx.cuh"
 
 namespace sq {
@@ -147,34 +148,6 @@ __device__ __forceinline__ void route_place(const int* base, const int32_t* ids,
       row_token[r] = static_cast<int32_t>(i / k);
     }
   }
-}
-
-// Exclusive scan of v over the block's threads; `warp_sums`: 33 ints.  Returns the sum before this thread; total in warp_sums[32].
-__device__ __forceinline__ int block_scan(int v, int* warp_sums) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  int s = v;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int u = __shfl_up_sync(0xFFFFFFFFu, s, o);
-    if (lane >= o) s += u;
-  }
-  __syncthreads();
-  if (lane == 31) warp_sums[warp] = s;
-  __syncthreads();
-  if (warp == 0) {
-    const int nw = blockDim.x >> 5;
-    int w = lane < nw ? warp_sums[lane] : 0;
-    const int own = w;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xFFFFFFFFu, w, o);
-      if (lane >= o) w += u;
-    }
-    if (lane == 31) warp_sums[32] = w;
-    warp_sums[lane] = w - own;
-  }
-  __syncthreads();
-  return warp_sums[warp] + s - v;
 }
 
 __device__ __forceinline__ double block_sum(double v, double* sums) {
