@@ -1,6 +1,7 @@
 // Weight-only products with group scales:
 //   w[c, k] = code[c, k] * sg[k / group, c] + bg[k / group, c],   Y[r, c] = fp16(sum_k Z16[token(r), k] * w_e(r)[c, k])
 // for one matrix of weights (dense) or for the experts of a sparse block, whose rows the router sorted on the device.
+#include <cuda.h>
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -63,64 +64,108 @@ gs_simple_kernel(const GsArgs a) {
 // channels; the eight warps of a block split K, in steps of 128 channels dealt out in turn.  Two blocks share an SM, so that one
 // streams while the other adds up, and so that the next kernel's first weights are on their way before this one ends.
 //
-// Every thread copies from global memory what it alone will read: lane 4 g + t takes the 16-byte piece t of the rows 2 g and 2 g + 1
-// of a block of 16 (an MMA's rows g and g + 8, in whatever order of k as long as weights and tokens agree), and the fp16 pair of
-// their scales.  So a warp's ring needs no barrier, only the thread's own wait for its copies, and it runs on from tile to tile.
-// The tokens come straight from L2 into the MMA's layout, a step ahead: each warp needs another part of K, nothing is shared.
+// Each warp has a ring of its own in shared memory, filled by its own TMA loads (16 RB rows x 64 bytes): no barriers between warps,
+// and it runs on from tile to tile.  The tokens come straight from L2 into the MMA's layout, eight rows ahead: each warp needs
+// another part of K.  (With 16-byte asynchronous copies in place of TMA a step of 16 x 128 weights took 169 instructions.)
 //
-// The weight is code * scale + offset in one fp16 fused multiply-add (one rounding, 2^-11 of the weight); sums are fp32.  With
-// steps of one group (128) the scale could follow the MMAs in fp32, but not with 32 or 64, whose pieces meet in one MMA.
+// A nibble is not widened at all: masked out of its word it IS the fp16 subnormal v 2^-24 (bits 0 to 3) or v 2^-20 (bits 4 to 7), v =
+// code + 8, which the MMA multiplies exactly.  One shift by 8 and four logic operations make eight weights.  Products with the
+// two kinds go to accumulators of their own, and behind each group, in fp32,
+//   sum += scale 2^24 (lo + hi / 16) + (offset - 8 scale) sum(x),
+// with the group's sum of the tokens from an MMA with ones, once for all channels of the warp.  No weight is rounded.  (With each
+// weight made fp16(code scale + offset) beforehand -- 13 operations for eight weights in place of 5 -- 1 x 4096 -> 14336 took 10.7 us.)
+//
+// So that an MMA stays within a group of 32, 64 or 128, lane 4 g + t takes word t, words 2 t, 2 t + 1 or piece t (four words) of
+// the group: the MMA's order of k is whatever weights and tokens agree on.
 constexpr int GS_WARPS = 8, GS_THREADS = GS_WARPS * 32;
 
-template <int RB, int NT, bool BIAS>
+template <int RB, int NT, int GROUP>
 struct GsStream {
-  static constexpr int SLOT = 1024 + (BIAS ? 256 : 128);      // 16 channels x 128 codes, their scales (and offsets), per lane
-  static constexpr int DEPTH = RB == 1 ? 8 : (RB == 2 ? 4 : (RB == 3 ? 3 : 2));
-  static constexpr int RING = DEPTH * RB * SLOT;              // of a warp
-  static constexpr int PITCH = 16 * RB + 8;                   // of the sums: 2 pitch = 16 banks
+  static constexpr int CHUNKS = 128 / GROUP;                  // groups of a step
+  static constexpr int WPL = GROUP / 32;                      // words of a group that a lane takes
+  static constexpr int ROWS = 16 * RB;
+  static constexpr int DEPTH = RB == 1 ? 8 : (RB == 2 ? 4 : 2);
+  static constexpr int W_SLOT = ROWS * 64;                    // 128 codes of each row
+  static constexpr int S_SLOT = CHUNKS * ROWS * 2;            // the groups' scales, and as much for the offsets
+  static constexpr int OFF_S = DEPTH * W_SLOT;
+  static constexpr int RING = (OFF_S + 2 * DEPTH * S_SLOT + 511) / 512 * 512;       // of a warp (SWIZZLE_64B repeats after 512 bytes)
+  static constexpr int PITCH = ROWS + 4;                      // of the sums: 8 banks from a token pair to the next
   static constexpr int PART = 8 * NT * PITCH;                 // floats of one warp's sums
-  static constexpr int BYTES = GS_WARPS * (RING + 4 * PART);
+  static constexpr int OFF_PART = GS_WARPS * RING;
+  static constexpr int OFF_BAR = OFF_PART + GS_WARPS * 4 * PART;
+  static constexpr int BYTES = OFF_BAR + GS_WARPS * DEPTH * 8 + 512;                // slack for the alignment
   static_assert(BYTES <= 112 * 1024, "two blocks to an SM");
 };
+enum GsSite : uint32_t { GS_FULL = 112 };
 
-__device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, bool take) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
-}
 __device__ __forceinline__ void cp_async_4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ uint32_t lds32(uint32_t a) {
-  uint32_t v;
-  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
-  return v;
+__device__ __forceinline__ float lds_half(uint32_t a) {
+  unsigned short v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
+  return __half2float(__ushort_as_half(v));
 }
-__device__ __forceinline__ uint4 lds128_at(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-  return v;
+// D = A B: a sum that begins.
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
+template <int W>
+__device__ __forceinline__ void lds_words(uint32_t a, uint32_t (&w)[W]) {
+  if constexpr (W == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(a) : "memory");
+  else if constexpr (W == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(a) : "memory");
+  else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(a) : "memory");
+}
+// Nibbles as subnormals: (w & mask) ^ sign.  The constants come in registers, see widen_consts.
+struct NibbleConsts { uint32_t low, high; };
+__device__ __forceinline__ NibbleConsts nibble_consts() {
+  const uint32_t one = gridDim.y;                        // 1, which the compiler does not know
+  return {0x00080007u + one, 0x0080007Fu + one};
+}
+__device__ __forceinline__ uint32_t low_nibbles(uint32_t w, const NibbleConsts& k) {
+  uint32_t x;
+  asm("lop3.b32 %0, %1, 0x000F000F, %2, 0x6a;" : "=r"(x) : "r"(w), "r"(k.low));
+  return x;
+}
+__device__ __forceinline__ uint32_t high_nibbles(uint32_t w, const NibbleConsts& k) {
+  uint32_t x;
+  asm("lop3.b32 %0, %1, 0x00F000F0, %2, 0x6a;" : "=r"(x) : "r"(w), "r"(k.high));
+  return x;
 }
 
-template <int RB, int NT, bool BIAS, bool EXPERTS>
+template <int RB, int NT, int GROUP, bool EXPERTS>
 __global__ void __launch_bounds__(GS_THREADS, 2)
-gs_stream_kernel(const __grid_constant__ GsArgs a, int R, int splits) {
-  using L = GsStream<RB, NT, BIAS>;
+gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ GsArgs a, int R, int splits) {
+  using L = GsStream<RB, NT, GROUP>;
+  constexpr int CHUNKS = L::CHUNKS, WPL = L::WPL;
   griddep_launch_dependents();
-  extern __shared__ __align__(16) unsigned char gs_smem[];
+  extern __shared__ unsigned char smem_dyn[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 511) & ~uintptr_t(511));
   __shared__ int first[EXPERTS ? 1025 : 1];
-  float* part = reinterpret_cast<float*>(gs_smem + GS_WARPS * L::RING);
+  float* part = reinterpret_cast<float*>(smem + L::OFF_PART);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int K = a.K, N = static_cast<int>(a.N), group = a.group;
-  const int G = (K + group - 1) / group;
+  const int K = a.K, N = static_cast<int>(a.N);
+  const int G = (K + GROUP - 1) / GROUP;
   const int crank = splits > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   const int cid = static_cast<int>(blockIdx.x) / splits, ncl = static_cast<int>(gridDim.x) / splits;
   const int nks = (K + 127) / 128;
   const int ks0 = crank * nks / splits + warp, ks1 = (crank + 1) * nks / splits;
   const int cw = ks1 > ks0 ? (ks1 - ks0 + GS_WARPS - 1) / GS_WARPS : 0;      // this warp's steps of a tile
   const int ctiles = (N + R - 1) / R;
+  unsigned char* ring = smem + warp * L::RING;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR) + warp * L::DEPTH;
+  if (lane == 0) {
+#pragma unroll
+    for (int d = 0; d < L::DEPTH; ++d) mbar_init(&full[d], 1);
+    mbar_fence_init();
+  }
+  __syncwarp();
   int tiles = ctiles;
   if constexpr (EXPERTS) {
     griddep_wait();                                  // the offsets come from the router
@@ -129,39 +174,46 @@ gs_stream_kernel(const __grid_constant__ GsArgs a, int R, int splits) {
   }
   const int my_tiles = cid < tiles ? (tiles - cid + ncl - 1) / ncl : 0;
   const int total = my_tiles * cw;
-  const uint32_t ring = smem_u32(gs_smem) + warp * L::RING + lane * 16;
-  const uint32_t ring_s = smem_u32(gs_smem) + warp * L::RING + 1024 + lane * 4;
+  const uint32_t limit = wait_limit();
+
+  // Where this lane reads its words of row g of a block, by group: 16-byte piece p of row r lies at p ^ (r >> 1 & 3).
+  uint32_t take[CHUNKS];
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    const int word = c * (GROUP / 8) + t * WPL;      // of the row's sixteen
+    take[c] = smem_u32(ring) + g * 64 + (((word >> 2) ^ (g >> 1 & 3)) << 4) + (word & 3) * 4;
+  }
+  const uint32_t take_s = smem_u32(ring) + L::OFF_S + g * 2;
 
   // Cursor of the copies: step `iq` of the sequence, its tile's weights.
-  int iq = 0, iks = ks0, itile = cid, islot = 0;
-  const uint8_t* iw = nullptr;
-  const __half *is = nullptr, *ib = nullptr;
-  int irows = 0;
-  auto aim = [&]() {
-    const int chunk = EXPERTS ? itile / ctiles : 0;
-    const int e = EXPERTS ? chunk_expert(first, a.E, chunk) : 0;
-    const int row0 = (itile - chunk * ctiles) * R;
-    irows = min(R, N - row0);
-    iw = a.Wq + (static_cast<size_t>(e) * N + row0 + 2 * g) * (K / 2) + 16 * t;
-    is = a.sg + static_cast<size_t>(e) * G * N + row0;
-    if (BIAS) ib = a.bg + static_cast<size_t>(e) * G * N + row0;
-  };
+  int iq = 0, iks = ks0, itile = cid, islot = 0, iy = 0;
+  const __half *is = nullptr, *ib = nullptr;         // scales of this lane's pair of channels
+  bool iin = false;
   auto issue = [&]() {
     if (iq < total) {
-      if (iks == ks0) aim();
-      const int k = iks * 128 + 32 * t;
-      const size_t gi = static_cast<size_t>(min(k, K - 1) / group) * N;
+      if (iks == ks0) {
+        const int chunk = EXPERTS ? itile / ctiles : 0;
+        const int e = EXPERTS ? chunk_expert(first, a.E, chunk) : 0;
+        const int row0 = (itile - chunk * ctiles) * R;
+        iy = e * N + row0;
+        iin = 2 * lane < min(R, N - row0);
+        const size_t so = static_cast<size_t>(e) * G * N + row0 + 2 * lane;
+        is = a.sg + so;
+        ib = a.bg + so;
+      }
+      if (lane == 0) {
+        mbar_arrive_expect_tx(&full[islot], static_cast<uint32_t>(R * 64));
+        tma_load_2d(ring + islot * L::W_SLOT, &tmap_w, &full[islot], iks * 64, iy);
+      }
+      if (iin) {
 #pragma unroll
-      for (int b = 0; b < RB; ++b) {
-        const int r = 16 * b + 2 * g;
-        const bool ok = r < irows && k < K;
-        const uint8_t* w = ok ? iw + static_cast<size_t>(16 * b) * (K / 2) + iks * 64 : a.Wq;
-        const uint32_t d = (islot * RB + b) * L::SLOT;
-        cp_async_16(ring + d, w, ok);
-        cp_async_16(ring + d + 512, ok ? w + K / 2 : a.Wq, ok);
-        const size_t si = gi + min(r, irows - 2);
-        cp_async_4(ring_s + d, is + si);
-        if (BIAS) cp_async_4(ring_s + d + 128, ib + si);
+        for (int c = 0; c < CHUNKS; ++c) {
+          // (A group behind the last one takes the last one's: its tokens are zeros, its scales have to be finite.)
+          const size_t o = static_cast<size_t>(min(iks * CHUNKS + c, G - 1)) * N;
+          const uint32_t d = smem_u32(ring) + L::OFF_S + (islot * 2 * CHUNKS + c) * (2 * L::ROWS) + lane * 4;
+          cp_async_4(d, is + o);
+          if (a.bg != nullptr) cp_async_4(d + L::S_SLOT, ib + o);
+        }
       }
       iks += GS_WARPS;
       if (iks >= ks1) {
@@ -177,13 +229,14 @@ gs_stream_kernel(const __grid_constant__ GsArgs a, int R, int splits) {
   for (int d = 0; d < L::DEPTH; ++d) issue();
   if constexpr (!EXPERTS) griddep_wait();            // Z16 may come from the kernel before, which may still read Y
 
-  // Cursor of the tokens, a step ahead of the products.
-  int xq = 0, xks = ks0, xtile = cid;
+  // Cursor of the tokens, eight rows ahead of the products.  Columns of an MMA that are no row of the tile repeat another row (its
+  // sums are not stored).
+  int xq = 0, xks = ks0, xtile = cid, xset = 0;
   const __half* xrow[NT];
-  uint4 xn[NT][4];
+  uint4 xn[4];
   auto fetch = [&]() {
     if (xq < total) {
-      if (xks == ks0 && (EXPERTS || xq == 0)) {
+      if (xset == 0 && xks == ks0 && (EXPERTS || xq == 0)) {
         long long lo = 0, hi = a.M;
         if constexpr (EXPERTS) {
           const int chunk = xtile / ctiles, e = chunk_expert(first, a.E, chunk);
@@ -192,31 +245,46 @@ gs_stream_kernel(const __grid_constant__ GsArgs a, int R, int splits) {
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const long long r = lo + 8 * n + g;
-          long long tok = -1;
-          if (r < hi) tok = EXPERTS && a.row_token != nullptr ? a.row_token[r] : r;
-          xrow[n] = tok >= 0 && tok < a.T ? a.Z + static_cast<size_t>(tok) * K + 32 * t : nullptr;
+          long long tok = lo + 8 * n + g;
+          tok = tok < hi ? tok : hi - 1;
+          if (EXPERTS && a.row_token != nullptr) tok = a.row_token[tok];
+          tok = tok < 0 ? 0 : (tok < a.T ? tok : a.T - 1);       // (no such token: zeros are stored, see below)
+          xrow[n] = a.Z + static_cast<size_t>(tok) * K + 8 * WPL * t;
         }
       }
+      const __half* row = (NT == 2 && xset == 1 ? xrow[NT - 1] : xrow[0]) + xks * 128;
+      if (xks * 128 + 128 <= K) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+        for (int i = 0; i < 4; ++i)                  // word i % WPL of chunk i / WPL
+          xn[i] = __ldg(reinterpret_cast<const uint4*>(row + (i / WPL) * GROUP + 8 * (i % WPL)));
+      } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          xn[n][i] = xrow[n] != nullptr && xks * 128 + 32 * t < K ? __ldg(reinterpret_cast<const uint4*>(xrow[n] + xks * 128) + i)
-                                                                  : make_uint4(0u, 0u, 0u, 0u);
-      xks += GS_WARPS;
-      if (xks >= ks1) {
-        xks = ks0;
-        xtile += ncl;
+        for (int i = 0; i < 4; ++i) {
+          const int k = (i / WPL) * GROUP + 8 * (i % WPL);
+          xn[i] = xks * 128 + k + 8 * WPL * t < K ? __ldg(reinterpret_cast<const uint4*>(row + k)) : make_uint4(0u, 0u, 0u, 0u);
+        }
       }
-      ++xq;
+      if (++xset == NT) {
+        xset = 0;
+        xks += GS_WARPS;
+        if (xks >= ks1) {
+          xks = ks0;
+          xtile += ncl;
+        }
+        ++xq;
+      }
     }
   };
   fetch();
 
-  const WidenConsts wk = widen_consts();
+  const NibbleConsts nk = nibble_consts();
+  const uint32_t ones = 0x3C003C00u;
   int slot = 0;
+  uint32_t phase = 0;
+  bool ok = true;
   for (int tl = 0, tile = cid; tl < my_tiles; ++tl, tile += ncl) {
+    const int chunk = EXPERTS ? tile / ctiles : 0;
+    const int row0 = (tile - chunk * ctiles) * R, rows = min(R, N - row0);
     float acc[RB][NT][4];
 #pragma unroll
     for (int b = 0; b < RB; ++b)
@@ -225,32 +293,80 @@ gs_stream_kernel(const __grid_constant__ GsArgs a, int R, int splits) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[b][n][e] = 0.0f;
     for (int i = 0; i < cw; ++i) {
-      uint4 x[NT][4];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[n][j] = xn[n][j];
-      fetch();
-      cp_async_wait<L::DEPTH - 1>();
-#pragma unroll
-      for (int b = 0; b < RB; ++b) {
-        const uint32_t d = (slot * RB + b) * L::SLOT;
-        const uint4 u = lds128_at(ring + d), v = lds128_at(ring + d + 512);
-        const uint32_t sw = lds32(ring_s + d), bw = BIAS ? lds32(ring_s + d + 128) : 0u;
-        const __half2 sh = *reinterpret_cast<const __half2*>(&sw), bh = *reinterpret_cast<const __half2*>(&bw);
-        const __half2 s0 = __low2half2(sh), s1 = __high2half2(sh), b0 = __low2half2(bh), b1 = __high2half2(bh);
+      for (int n = 0; n < NT; ++n) {                 // (16 rows: the nibbles are masked out twice, which costs less than 32 more registers)
+        // Channel pairs (0, 1) and (4, 5) of each word, then (2, 3) and (6, 7): as the MMAs take them.
+        uint2 xl[4], xh[4];
+        float2 sx[CHUNKS];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint4 p = scaled_word<BIAS>(word_of(u, j), wk, s0, b0), q = scaled_word<BIAS>(word_of(v, j), wk, s1, b1);
+          xl[j] = make_uint2(xn[j].x, xn[j].z);
+          xh[j] = make_uint2(xn[j].y, xn[j].w);
+        }
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            mma_f16(acc[b][n], p.x, q.x, p.y, q.y, x[n][j].x, x[n][j].y);
-            mma_f16(acc[b][n], p.z, q.z, p.w, q.w, x[n][j].z, x[n][j].w);
+        for (int c = 0; c < CHUNKS; ++c) {
+          float d[4];
+#pragma unroll
+          for (int j = 0; j < WPL; ++j) {
+            const uint2 vl = xl[c * WPL + j], vh = xh[c * WPL + j];
+            if (j == 0) mma_f16_first(d, ones, ones, ones, ones, vl.x, vl.y);
+            else mma_f16(d, ones, ones, ones, ones, vl.x, vl.y);
+            mma_f16(d, ones, ones, ones, ones, vh.x, vh.y);
+          }
+          sx[c] = make_float2(d[0], d[1]);
+        }
+        fetch();
+        if (n == 0) {
+          cp_async_wait<L::DEPTH - 1>();
+          // (After a time-out nothing is requested any more, and what is on its way gets a little longer.)
+          ok = mbar_wait(&full[slot], phase, GS_FULL, ok ? limit : 65536u) && ok;
+          __syncwarp();                              // the other lanes' scales
+        }
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+          if (RB > 1 && 16 * b >= rows) break;
+          const uint32_t d = slot * L::W_SLOT + b * 1024, ds = slot * 2 * L::S_SLOT + b * 32;
+#pragma unroll
+          for (int c = 0; c < CHUNKS; ++c) {
+            uint32_t u[WPL], v[WPL];
+            lds_words<WPL>(take[c] + d, u);
+            lds_words<WPL>(take[c] + d + 512, v);
+            const uint32_t sa = take_s + ds + c * (2 * L::ROWS);
+            const float2 s = make_float2(lds_half(sa), lds_half(sa + 16));
+            float2 o = make_float2(0.0f, 0.0f);
+            if (a.bg != nullptr) o = make_float2(lds_half(sa + L::S_SLOT), lds_half(sa + L::S_SLOT + 16));
+            float lo[4], hi[4];
+#pragma unroll
+            for (int j = 0; j < WPL; ++j) {
+              const uint32_t u8 = u[j] >> 8, v8 = v[j] >> 8;
+              const uint2 p = xl[c * WPL + j], q = xh[c * WPL + j];
+              const uint32_t ul = low_nibbles(u[j], nk), vl = low_nibbles(v[j], nk), ul8 = low_nibbles(u8, nk), vl8 = low_nibbles(v8, nk);
+              const uint32_t uh = high_nibbles(u[j], nk), vh = high_nibbles(v[j], nk), uh8 = high_nibbles(u8, nk), vh8 = high_nibbles(v8, nk);
+              if (j == 0) {
+                mma_f16_first(lo, ul, vl, ul8, vl8, p.x, p.y);
+                mma_f16_first(hi, uh, vh, uh8, vh8, q.x, q.y);
+              } else {
+                mma_f16(lo, ul, vl, ul8, vl8, p.x, p.y);
+                mma_f16(hi, uh, vh, uh8, vh8, q.x, q.y);
+              }
+            }
+            const float s0 = s.x * 16777216.0f, s1 = s.y * 16777216.0f, o0 = fmaf(-8.0f, s.x, o.x), o1 = fmaf(-8.0f, s.y, o.y);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {            // e & 1: token 2 t or 2 t + 1, e >> 1: channel g or g + 8
+              const float sum = fmaf(hi[e], 0.0625f, lo[e]);
+              acc[b][n][e] = fmaf(e < 2 ? s0 : s1, sum, acc[b][n][e]);
+              acc[b][n][e] = fmaf(e < 2 ? o0 : o1, (e & 1) ? sx[c].y : sx[c].x, acc[b][n][e]);
+            }
           }
         }
       }
-      if (++slot == L::DEPTH) slot = 0;
-      issue();
+      if (++slot == L::DEPTH) {
+        slot = 0;
+        phase ^= 1;
+      }
+      __syncwarp();                                  // every lane has read the slot
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (ok) issue();
     }
     // The warps' sums over K, added up in a fixed order.
     float* mine = part + warp * L::PART;
@@ -258,18 +374,19 @@ gs_stream_kernel(const __grid_constant__ GsArgs a, int R, int splits) {
     for (int b = 0; b < RB; ++b)
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        *reinterpret_cast<float2*>(mine + (8 * n + 2 * t) * L::PITCH + 16 * b + 2 * g) = make_float2(acc[b][n][0], acc[b][n][2]);
-        *reinterpret_cast<float2*>(mine + (8 * n + 2 * t + 1) * L::PITCH + 16 * b + 2 * g) = make_float2(acc[b][n][1], acc[b][n][3]);
+        float* p = mine + (8 * n + 2 * t) * L::PITCH + 16 * b + g;
+        p[0] = acc[b][n][0];
+        p[L::PITCH] = acc[b][n][1];
+        p[8] = acc[b][n][2];
+        p[L::PITCH + 8] = acc[b][n][3];
       }
     __syncthreads();
-    const int chunk = EXPERTS ? tile / ctiles : 0;
     long long r0 = 0, r1 = a.M;
     if constexpr (EXPERTS) {
       const int e = chunk_expert(first, a.E, chunk);
       expert_rows(a, e, r0, r1);
       r0 += static_cast<long long>(chunk - first[e]) * (8 * NT);
     }
-    const int row0 = (tile - chunk * ctiles) * R, rows = min(R, N - row0);
     for (int o = threadIdx.x; o < 64 * RB * NT; o += GS_THREADS) {
       const int tok = o / (8 * RB), c = 2 * (o % (8 * RB));
       float* p = part + tok * L::PITCH + c;
@@ -281,8 +398,13 @@ gs_stream_kernel(const __grid_constant__ GsArgs a, int R, int splits) {
         v.y += u.y;
       }
       if (splits > 1) *reinterpret_cast<float2*>(p) = v;       // the first warp's place: this thread alone reads it here
-      else if (c < rows && r0 + tok < r1)
+      else if (c < rows && r0 + tok < r1) {
+        if (EXPERTS && a.row_token != nullptr) {
+          const long long id = a.row_token[r0 + tok];
+          if (id < 0 || id >= a.T) v = make_float2(0.0f, 0.0f);
+        }
         *reinterpret_cast<__half2*>(a.Y + static_cast<size_t>(r0 + tok) * N + row0 + c) = __floats2half2_rn(v.x, v.y);
+      }
     }
     if (splits > 1) {
       // One tile per cluster then.  Block r of it finishes every splits-th pair of channels.
@@ -398,32 +520,41 @@ sq_status_t launch_quant_groups(const void* X, bool f32, int64_t rows, int64_t r
 
 namespace {
 
-template <int RB, int NT, bool BIAS, bool EXPERTS>
+template <int RB, int NT, int GROUP, bool EXPERTS>
 sq_status_t launch_stream_as(const GsArgs& a, int R, int splits, int grid, cudaStream_t s) {
-  using L = GsStream<RB, NT, BIAS>;
-  auto kern = gs_stream_kernel<RB, NT, BIAS, EXPERTS>;
+  using L = GsStream<RB, NT, GROUP>;
+  auto kern = gs_stream_kernel<RB, NT, GROUP, EXPERTS>;
   if (!ensure_dyn_smem(reinterpret_cast<const void*>(kern), L::BYTES)) return SQ_ERR_CUDA;
+  EncodeTiledFn enc = get_encode_fn();
+  if (!enc) return SQ_ERR_CUDA;
+  CUtensorMap mw;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(a.K / 2), static_cast<cuuint64_t>(a.N * std::max(a.E, 1))};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(a.K / 2)};
+  const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(R)};
+  const cuuint32_t estr[2] = {1, 1};
+  if (enc(&mw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(a.Wq), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+          CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return SQ_ERR_CUDA;
   const cudaError_t err = launch_cluster_maybe_pdl(kern, dim3(static_cast<unsigned>(grid)), dim3(GS_THREADS), static_cast<size_t>(L::BYTES),
-                                                   s, static_cast<unsigned>(splits), a, R, splits);
+                                                   s, static_cast<unsigned>(splits), mw, a, R, splits);
   count_launch();
   return err == cudaSuccess ? SQ_OK : SQ_ERR_CUDA;
 }
-template <int NT, bool BIAS, bool EXPERTS>
+template <int NT, int GROUP, bool EXPERTS>
 sq_status_t launch_stream_rows(const GsArgs& a, int R, int splits, int grid, cudaStream_t s) {
-  if (R <= 16) return launch_stream_as<1, NT, BIAS, EXPERTS>(a, R, splits, grid, s);
-  if (R <= 32) return launch_stream_as<2, NT, BIAS, EXPERTS>(a, R, splits, grid, s);
-  if constexpr (NT == 1) {
-    if (R <= 48) return launch_stream_as<3, NT, BIAS, EXPERTS>(a, R, splits, grid, s);
-    return launch_stream_as<4, NT, BIAS, EXPERTS>(a, R, splits, grid, s);
-  }
+  if (R <= 16) return launch_stream_as<1, NT, GROUP, EXPERTS>(a, R, splits, grid, s);
+  if (R <= 32) return launch_stream_as<2, NT, GROUP, EXPERTS>(a, R, splits, grid, s);
+  if constexpr (NT == 1) return launch_stream_as<4, NT, GROUP, EXPERTS>(a, R, splits, grid, s);
   return SQ_ERR_UNSUPPORTED;
 }
 template <bool EXPERTS>
 sq_status_t launch_stream_any(const GsArgs& a, int nt, int R, int splits, int grid, cudaStream_t s) {
-  if (nt == 1) return a.bg ? launch_stream_rows<1, true, EXPERTS>(a, R, splits, grid, s) : launch_stream_rows<1, false, EXPERTS>(a, R, splits, grid, s);
-  return a.bg ? launch_stream_rows<2, true, EXPERTS>(a, R, splits, grid, s) : launch_stream_rows<2, false, EXPERTS>(a, R, splits, grid, s);
+  if (a.group == 128) return nt == 1 ? launch_stream_rows<1, 128, EXPERTS>(a, R, splits, grid, s) : launch_stream_rows<2, 128, EXPERTS>(a, R, splits, grid, s);
+  if (a.group == 64) return nt == 1 ? launch_stream_rows<1, 64, EXPERTS>(a, R, splits, grid, s) : launch_stream_rows<2, 64, EXPERTS>(a, R, splits, grid, s);
+  return nt == 1 ? launch_stream_rows<1, 32, EXPERTS>(a, R, splits, grid, s) : launch_stream_rows<2, 32, EXPERTS>(a, R, splits, grid, s);
 }
 
+constexpr double GS_SPLIT_COST = 6.0;
 int even_rows(int64_t N, int64_t tiles) { return static_cast<int>(std::max<int64_t>(2, (N + 2 * tiles - 1) / (2 * tiles) * 2)); }
 
 sq_status_t launch_stream(const GsArgs& a, cudaStream_t s) {
@@ -439,20 +570,23 @@ sq_status_t launch_stream(const GsArgs& a, cudaStream_t s) {
     return launch_stream_any<true>(a, nt, R, 1, slots, s);
   }
   const int nt = a.M <= 8 ? 1 : 2, cap = nt == 1 ? 64 : 32;
-  // A block's bytes, weights and tokens, with K in 1, 2, 4 or 8 parts.
+  // Time of a tile's step of 128 channels, in steps of 16 channels: its blocks of 16, its tokens and what a step costs by itself; for
+  // the tiles that a block gets, with K in 1, 2, 4 or 8 parts.
   int best_r = 0, best_s = 1, best_grid = 0;
   double best = 0.0;
-  for (int sp = 1; sp <= 8 && nks / sp >= (sp == 1 ? 1 : 4); sp *= 2) {
-    const int R = std::min(cap, even_rows(a.N, slots / sp));
-    const int64_t tiles = (a.N + R - 1) / R;
-    if (sp > 1 && tiles * sp > slots) continue;
-    const int64_t waves = (tiles * sp + slots - 1) / slots;
-    const double cost = static_cast<double>(waves) * ((nks + sp - 1) / sp) * (R * 64.0 + a.M * 256.0) + (sp > 1 ? 20000.0 : 0.0);
-    if (best_r == 0 || cost < best) {
-      best = cost;
-      best_r = R;
-      best_s = sp;
-      best_grid = static_cast<int>(std::min<int64_t>(tiles * sp, slots));
+  for (int sp = 1; sp <= 8 && nks / sp >= (sp == 1 ? 1 : 8); sp *= 2) {
+    for (int waves = 1; waves <= (sp == 1 ? 8 : 1); ++waves) {
+      const int R = even_rows(a.N, static_cast<int64_t>(slots / sp) * waves);
+      if (R > cap && (sp > 1 || waves < 8)) continue;
+      const int r = std::min(R, cap);
+      const int64_t tiles = (a.N + r - 1) / r, rounds = (tiles * sp + slots - 1) / slots;
+      const double cost = static_cast<double>(rounds) * (((nks + sp - 1) / sp + 7) / 8) * ((r + 15) / 16 + 0.5 + 0.1 * a.M) + (sp > 1 ? GS_SPLIT_COST : 0.0);
+      if (best_r == 0 || cost < best) {
+        best = cost;
+        best_r = r;
+        best_s = sp;
+        best_grid = static_cast<int>(std::min<int64_t>(tiles * sp, slots));
+      }
     }
   }
   return launch_stream_any<false>(a, nt, best_r, best_s, best_grid, s);
@@ -480,9 +614,8 @@ int gs_tile_m(const GsArgs& a) {
 
 sq_status_t launch_gemm_gs(const GsArgs& a, void* workspace, cudaStream_t s) {
   const bool few = a.E > 0 ? a.M <= 16 * static_cast<int64_t>(a.E) : a.M <= 16;
-  if (a.K % 32 == 0 && a.N % 2 == 0 && few) return launch_stream(a, s);
-  // (32-bit coordinates of a tile in the weights and in the rows)
-  const int64_t kMax = (1ll << 31) - 1024;
+  const int64_t kMax = (1ll << 31) - 1024;           // 32-bit coordinates of a tile in the weights and in the rows
+  if (a.K % 32 == 0 && a.N % 2 == 0 && few && a.N * std::max(a.E, 1) <= kMax) return launch_stream(a, s);
   if (a.K % 32 == 0 && a.M <= kMax && a.N * std::max(a.E, 1) <= kMax) {
     if (a.E == 0) return launch_wo_gemm_groups(a, 0, s);
     GsArgs b = a;
