@@ -71,8 +71,9 @@ gs_simple_kernel(const GsArgs a) {
 // A nibble is not widened at all: masked out of its word it IS the fp16 subnormal v 2^-24 (bits 0 to 3) or v 2^-20 (bits 4 to 7), v =
 // code + 8, which the MMA multiplies exactly.  One shift by 8 and four logic operations make eight weights.  Products with the
 // two kinds go to accumulators of their own, and behind each group, in fp32,
-//   sum += scale 2^24 (lo + hi / 16) + (offset - 8 scale) sum(x),
-// with the group's sum of the tokens from an MMA with ones, once for all channels of the warp.  No weight is rounded.  (With each
+//   sum += scale (lo - 8 sum(x) + hi / 16) + offset sum(x)      (in units of 2^-24),
+// with the group's sum of the tokens from an MMA with ones, once for all channels of the warp; -8 sum(x) is what lo begins with.  No
+// weight is rounded.  (With each
 // weight made fp16(code scale + offset) beforehand -- 13 operations for eight weights in place of 5 -- 1 x 4096 -> 14336 took 10.7 us.)
 //
 // So that an MMA stays within a group of 32, 64 or 128, lane 4 g + t takes word t, words 2 t, 2 t + 1 or piece t (four words) of
@@ -109,7 +110,7 @@ __device__ __forceinline__ float lds_half(uint32_t a) {
   asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
   return __half2float(__ushort_as_half(v));
 }
-// D = A B: a sum that begins.
+// D = A B, or A B + (c0, c1) in both halves of the rows: sums that begin.
 __device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
@@ -122,6 +123,12 @@ __device__ __forceinline__ void lds_words(uint32_t a, uint32_t (&w)[W]) {
   else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(a) : "memory");
 }
 // Nibbles as subnormals: (w & mask) ^ sign.  The constants come in registers, see widen_consts.
+__device__ __forceinline__ void mma_f16_from(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1,
+                                             float c0, float c1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%10,%11};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+}
 struct NibbleConsts { uint32_t low, high; };
 __device__ __forceinline__ NibbleConsts nibble_consts() {
   const uint32_t one = gridDim.y;                        // 1, which the compiler does not know
@@ -138,7 +145,7 @@ __device__ __forceinline__ uint32_t high_nibbles(uint32_t w, const NibbleConsts&
   return x;
 }
 
-template <int RB, int NT, int GROUP, bool EXPERTS>
+template <int RB, int NT, int GROUP, bool BIAS, bool EXPERTS>
 __global__ void __launch_bounds__(GS_THREADS, 2)
 gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ GsArgs a, int R, int splits) {
   using L = GsStream<RB, NT, GROUP>;
@@ -149,7 +156,7 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
   __shared__ int first[EXPERTS ? 1025 : 1];
   float* part = reinterpret_cast<float*>(smem + L::OFF_PART);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x) >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int K = a.K, N = static_cast<int>(a.N);
   const int G = (K + GROUP - 1) / GROUP;
   const int crank = splits > 1 ? static_cast<int>(cluster_ctarank()) : 0;
@@ -157,6 +164,8 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
   const int nks = (K + 127) / 128;
   const int ks0 = crank * nks / splits + warp, ks1 = (crank + 1) * nks / splits;
   const int cw = ks1 > ks0 ? (ks1 - ks0 + GS_WARPS - 1) / GS_WARPS : 0;      // this warp's steps of a tile
+  // The step whose channels end before 128 of them, if it is this warp's: always the last of its steps.
+  const bool ragged = (K & 127) != 0 && cw > 0 && ks0 + (cw - 1) * GS_WARPS == nks - 1;
   const int ctiles = (N + R - 1) / R;
   unsigned char* ring = smem + warp * L::RING;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR) + warp * L::DEPTH;
@@ -173,7 +182,6 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
     tiles = first[a.E] * ctiles;
   }
   const int my_tiles = cid < tiles ? (tiles - cid + ncl - 1) / ncl : 0;
-  const int total = my_tiles * cw;
   const uint32_t limit = wait_limit();
 
   // Where this lane reads its words of row g of a block, by group: 16-byte piece p of row r lies at p ^ (r >> 1 & 3).
@@ -185,43 +193,55 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
   }
   const uint32_t take_s = smem_u32(ring) + L::OFF_S + g * 2;
 
-  // Cursor of the copies: step `iq` of the sequence, its tile's weights.
-  int iq = 0, iks = ks0, itile = cid, islot = 0, iy = 0;
-  const __half *is = nullptr, *ib = nullptr;         // scales of this lane's pair of channels
+  // Cursor of the copies: the steps left of its tile, and the tile's weights and scales (of this lane's pair of channels).
+  int ileft = 0, itiles = cw > 0 ? my_tiles : 0, itile = cid, islot = 0, ix = 0, iy = 0;
+  const __half *is = nullptr, *ib = nullptr;
   bool iin = false;
+  const size_t step_s = static_cast<size_t>(GS_WARPS * CHUNKS) * N;
+  const uint32_t put_s = smem_u32(ring) + L::OFF_S + lane * 4;
   auto issue = [&]() {
-    if (iq < total) {
-      if (iks == ks0) {
-        const int chunk = EXPERTS ? itile / ctiles : 0;
-        const int e = EXPERTS ? chunk_expert(first, a.E, chunk) : 0;
-        const int row0 = (itile - chunk * ctiles) * R;
-        iy = e * N + row0;
-        iin = 2 * lane < min(R, N - row0);
-        const size_t so = static_cast<size_t>(e) * G * N + row0 + 2 * lane;
-        is = a.sg + so;
-        ib = a.bg + so;
-      }
+    if (ileft == 0 && itiles > 0) {
+      const int chunk = EXPERTS ? itile / ctiles : 0;
+      const int e = EXPERTS ? chunk_expert(first, a.E, chunk) : 0;
+      const int row0 = (itile - chunk * ctiles) * R;
+      iy = e * N + row0;
+      iin = 2 * lane < min(R, N - row0);
+      const size_t so = (static_cast<size_t>(e) * G + ks0 * CHUNKS) * N + row0 + 2 * lane;
+      is = a.sg + so;
+      if (BIAS) ib = a.bg + so;
+      ix = ks0 * 64;
+      ileft = cw;
+      itile += ncl;
+      --itiles;
+    }
+    if (ileft > 0) {
+      --ileft;
       if (lane == 0) {
         mbar_arrive_expect_tx(&full[islot], static_cast<uint32_t>(R * 64));
-        tma_load_2d(ring + islot * L::W_SLOT, &tmap_w, &full[islot], iks * 64, iy);
+        tma_load_2d(ring + islot * L::W_SLOT, &tmap_w, &full[islot], ix, iy);
       }
       if (iin) {
+        const uint32_t d = put_s + islot * (2 * L::S_SLOT);
+        if (!(ragged && ileft == 0)) {
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-          // (A group behind the last one takes the last one's: its tokens are zeros, its scales have to be finite.)
-          const size_t o = static_cast<size_t>(min(iks * CHUNKS + c, G - 1)) * N;
-          const uint32_t d = smem_u32(ring) + L::OFF_S + (islot * 2 * CHUNKS + c) * (2 * L::ROWS) + lane * 4;
-          cp_async_4(d, is + o);
-          if (a.bg != nullptr) cp_async_4(d + L::S_SLOT, ib + o);
+          for (int c = 0; c < CHUNKS; ++c) {
+            cp_async_4(d + c * (2 * L::ROWS), is + static_cast<size_t>(c) * N);
+            if (BIAS) cp_async_4(d + c * (2 * L::ROWS) + L::S_SLOT, ib + static_cast<size_t>(c) * N);
+          }
+        } else {
+          // A group behind the last one takes the last one's: its tokens are zeros, its scales have to be finite.
+#pragma unroll
+          for (int c = 0; c < CHUNKS; ++c) {
+            const size_t o = static_cast<size_t>(min(c, G - 1 - (nks - 1) * CHUNKS)) * N;
+            cp_async_4(d + c * (2 * L::ROWS), is + o);
+            if (BIAS) cp_async_4(d + c * (2 * L::ROWS) + L::S_SLOT, ib + o);
+          }
         }
       }
-      iks += GS_WARPS;
-      if (iks >= ks1) {
-        iks = ks0;
-        itile += ncl;
-      }
-      ++iq;
-      if (++islot == L::DEPTH) islot = 0;
+      is += step_s;
+      if (BIAS) ib += step_s;
+      ix += GS_WARPS * 64;
+      islot = islot + 1 == L::DEPTH ? 0 : islot + 1;
     }
     cp_async_commit();
   };
@@ -231,12 +251,13 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
 
   // Cursor of the tokens, eight rows ahead of the products.  Columns of an MMA that are no row of the tile repeat another row (its
   // sums are not stored).
-  int xq = 0, xks = ks0, xtile = cid, xset = 0;
-  const __half* xrow[NT];
+  int xleft = 0, xtiles = cw > 0 ? my_tiles : 0, xtile = cid;
+  const __half *xrow[NT], *xat[NT];
   uint4 xn[4];
-  auto fetch = [&]() {
-    if (xq < total) {
-      if (xset == 0 && xks == ks0 && (EXPERTS || xq == 0)) {
+  auto fetch = [&](int n) {
+    if (n == 0 && xleft == 0) {
+      if (xtiles == 0) return;
+      if (EXPERTS || xtile == cid) {
         long long lo = 0, hi = a.M;
         if constexpr (EXPERTS) {
           const int chunk = xtile / ctiles, e = chunk_expert(first, a.E, chunk);
@@ -244,38 +265,35 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
           lo += static_cast<long long>(chunk - first[e]) * (8 * NT);
         }
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          long long tok = lo + 8 * n + g;
+        for (int m = 0; m < NT; ++m) {
+          long long tok = lo + 8 * m + g;
           tok = tok < hi ? tok : hi - 1;
           if (EXPERTS && a.row_token != nullptr) tok = a.row_token[tok];
           tok = tok < 0 ? 0 : (tok < a.T ? tok : a.T - 1);       // (no such token: zeros are stored, see below)
-          xrow[n] = a.Z + static_cast<size_t>(tok) * K + 8 * WPL * t;
+          xrow[m] = a.Z + static_cast<size_t>(tok) * K + ks0 * 128 + 8 * WPL * t;
         }
       }
-      const __half* row = (NT == 2 && xset == 1 ? xrow[NT - 1] : xrow[0]) + xks * 128;
-      if (xks * 128 + 128 <= K) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)                  // word i % WPL of chunk i / WPL
-          xn[i] = __ldg(reinterpret_cast<const uint4*>(row + (i / WPL) * GROUP + 8 * (i % WPL)));
-      } else {
+      for (int m = 0; m < NT; ++m) xat[m] = xrow[m];
+      xleft = cw;
+      xtile += ncl;
+      --xtiles;
+    }
+    if (!(ragged && xleft == 1)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int k = (i / WPL) * GROUP + 8 * (i % WPL);
-          xn[i] = xks * 128 + k + 8 * WPL * t < K ? __ldg(reinterpret_cast<const uint4*>(row + k)) : make_uint4(0u, 0u, 0u, 0u);
-        }
-      }
-      if (++xset == NT) {
-        xset = 0;
-        xks += GS_WARPS;
-        if (xks >= ks1) {
-          xks = ks0;
-          xtile += ncl;
-        }
-        ++xq;
+      for (int i = 0; i < 4; ++i)                    // word i % WPL of chunk i / WPL
+        xn[i] = __ldg(reinterpret_cast<const uint4*>(xat[n] + (i / WPL) * GROUP + 8 * (i % WPL)));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int k = (i / WPL) * GROUP + 8 * (i % WPL);
+        xn[i] = (nks - 1) * 128 + k + 8 * WPL * t < K ? __ldg(reinterpret_cast<const uint4*>(xat[n] + k)) : make_uint4(0u, 0u, 0u, 0u);
       }
     }
+    xat[n] += GS_WARPS * 128;
+    if (n == NT - 1) --xleft;
   };
-  fetch();
+  fetch(0);
 
   const NibbleConsts nk = nibble_consts();
   const uint32_t ones = 0x3C003C00u;
@@ -285,7 +303,7 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
   for (int tl = 0, tile = cid; tl < my_tiles; ++tl, tile += ncl) {
     const int chunk = EXPERTS ? tile / ctiles : 0;
     const int row0 = (tile - chunk * ctiles) * R, rows = min(R, N - row0);
-    float acc[RB][NT][4];
+    float acc[RB][NT][4];                            // in units of 2^-24
 #pragma unroll
     for (int b = 0; b < RB; ++b)
 #pragma unroll
@@ -303,6 +321,7 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
           xl[j] = make_uint2(xn[j].x, xn[j].z);
           xh[j] = make_uint2(xn[j].y, xn[j].w);
         }
+        fetch((n + 1) % NT);
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
           float d[4];
@@ -313,50 +332,61 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
             else mma_f16(d, ones, ones, ones, ones, vl.x, vl.y);
             mma_f16(d, ones, ones, ones, ones, vh.x, vh.y);
           }
-          sx[c] = make_float2(d[0], d[1]);
+          sx[c] = make_float2(d[0] * 0x1p-24f, d[1] * 0x1p-24f);
         }
-        fetch();
         if (n == 0) {
           cp_async_wait<L::DEPTH - 1>();
           // (After a time-out nothing is requested any more, and what is on its way gets a little longer.)
           ok = mbar_wait(&full[slot], phase, GS_FULL, ok ? limit : 65536u) && ok;
           __syncwarp();                              // the other lanes' scales
         }
+        // Two blocks of 16 channels side by side: four chains of MMAs (a chain takes 21 cycles a link and up, the tensor pipe 8).
+        constexpr int PB = RB > 1 ? 2 : 1;
 #pragma unroll
-        for (int b = 0; b < RB; ++b) {
-          if (RB > 1 && 16 * b >= rows) break;
-          const uint32_t d = slot * L::W_SLOT + b * 1024, ds = slot * 2 * L::S_SLOT + b * 32;
+        for (int b0 = 0; b0 < RB; b0 += PB) {
+          if (RB > PB && 16 * b0 >= rows) break;
+          const uint32_t d = slot * L::W_SLOT + b0 * 1024, ds = take_s + slot * 2 * L::S_SLOT + b0 * 32;
 #pragma unroll
           for (int c = 0; c < CHUNKS; ++c) {
-            uint32_t u[WPL], v[WPL];
-            lds_words<WPL>(take[c] + d, u);
-            lds_words<WPL>(take[c] + d + 512, v);
-            const uint32_t sa = take_s + ds + c * (2 * L::ROWS);
-            const float2 s = make_float2(lds_half(sa), lds_half(sa + 16));
-            float2 o = make_float2(0.0f, 0.0f);
-            if (a.bg != nullptr) o = make_float2(lds_half(sa + L::S_SLOT), lds_half(sa + L::S_SLOT + 16));
-            float lo[4], hi[4];
+            uint32_t u[PB][WPL], v[PB][WPL];
+            float2 s[PB], o[PB];
+#pragma unroll
+            for (int b = 0; b < PB; ++b) {
+              lds_words<WPL>(take[c] + d + b * 1024, u[b]);
+              lds_words<WPL>(take[c] + d + b * 1024 + 512, v[b]);
+            }
+#pragma unroll
+            for (int b = 0; b < PB; ++b) {
+              const uint32_t sa = ds + c * (2 * L::ROWS) + b * 32;
+              s[b] = make_float2(lds_half(sa), lds_half(sa + 16));
+              if (BIAS) o[b] = make_float2(lds_half(sa + L::S_SLOT), lds_half(sa + L::S_SLOT + 16));
+            }
+            float lo[PB][4], hi[PB][4];
 #pragma unroll
             for (int j = 0; j < WPL; ++j) {
-              const uint32_t u8 = u[j] >> 8, v8 = v[j] >> 8;
               const uint2 p = xl[c * WPL + j], q = xh[c * WPL + j];
-              const uint32_t ul = low_nibbles(u[j], nk), vl = low_nibbles(v[j], nk), ul8 = low_nibbles(u8, nk), vl8 = low_nibbles(v8, nk);
-              const uint32_t uh = high_nibbles(u[j], nk), vh = high_nibbles(v[j], nk), uh8 = high_nibbles(u8, nk), vh8 = high_nibbles(v8, nk);
-              if (j == 0) {
-                mma_f16_first(lo, ul, vl, ul8, vl8, p.x, p.y);
-                mma_f16_first(hi, uh, vh, uh8, vh8, q.x, q.y);
-              } else {
-                mma_f16(lo, ul, vl, ul8, vl8, p.x, p.y);
-                mma_f16(hi, uh, vh, uh8, vh8, q.x, q.y);
+#pragma unroll
+              for (int b = 0; b < PB; ++b) {
+                const uint32_t uw = u[b][j], vw = v[b][j], u8 = uw >> 8, v8 = vw >> 8;
+                const uint32_t ul = low_nibbles(uw, nk), vl = low_nibbles(vw, nk), ul8 = low_nibbles(u8, nk), vl8 = low_nibbles(v8, nk);
+                const uint32_t uh = high_nibbles(uw, nk), vh = high_nibbles(vw, nk), uh8 = high_nibbles(u8, nk), vh8 = high_nibbles(v8, nk);
+                if (j == 0) {                        // -8 sum(x): v is code + 8
+                  mma_f16_from(lo[b], ul, vl, ul8, vl8, p.x, p.y, -8.0f * sx[c].x, -8.0f * sx[c].y);
+                  mma_f16_first(hi[b], uh, vh, uh8, vh8, q.x, q.y);
+                } else {
+                  mma_f16(lo[b], ul, vl, ul8, vl8, p.x, p.y);
+                  mma_f16(hi[b], uh, vh, uh8, vh8, q.x, q.y);
+                }
               }
             }
-            const float s0 = s.x * 16777216.0f, s1 = s.y * 16777216.0f, o0 = fmaf(-8.0f, s.x, o.x), o1 = fmaf(-8.0f, s.y, o.y);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {            // e & 1: token 2 t or 2 t + 1, e >> 1: channel g or g + 8
-              const float sum = fmaf(hi[e], 0.0625f, lo[e]);
-              acc[b][n][e] = fmaf(e < 2 ? s0 : s1, sum, acc[b][n][e]);
-              acc[b][n][e] = fmaf(e < 2 ? o0 : o1, (e & 1) ? sx[c].y : sx[c].x, acc[b][n][e]);
-            }
+            for (int b = 0; b < PB; ++b)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {          // e & 1: token 2 t or 2 t + 1, e >> 1: channel g or g + 8
+                float& sum = acc[b0 + b][n][e];
+                sum = fmaf(e < 2 ? s[b].x : s[b].y, fmaf(hi[b][e], 0.0625f, lo[b][e]), sum);
+                if (BIAS) sum = fmaf(e < 2 ? o[b].x : o[b].y, (e & 1) ? sx[c].y : sx[c].x, sum);
+              }
           }
         }
       }
@@ -375,10 +405,10 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         float* p = mine + (8 * n + 2 * t) * L::PITCH + 16 * b + g;
-        p[0] = acc[b][n][0];
-        p[L::PITCH] = acc[b][n][1];
-        p[8] = acc[b][n][2];
-        p[L::PITCH + 8] = acc[b][n][3];
+        p[0] = acc[b][n][0] * 0x1p24f;
+        p[L::PITCH] = acc[b][n][1] * 0x1p24f;
+        p[8] = acc[b][n][2] * 0x1p24f;
+        p[L::PITCH + 8] = acc[b][n][3] * 0x1p24f;
       }
     __syncthreads();
     long long r0 = 0, r1 = a.M;
@@ -520,10 +550,10 @@ sq_status_t launch_quant_groups(const void* X, bool f32, int64_t rows, int64_t r
 
 namespace {
 
-template <int RB, int NT, int GROUP, bool EXPERTS>
+template <int RB, int NT, int GROUP, bool BIAS, bool EXPERTS>
 sq_status_t launch_stream_as(const GsArgs& a, int R, int splits, int grid, cudaStream_t s) {
   using L = GsStream<RB, NT, GROUP>;
-  auto kern = gs_stream_kernel<RB, NT, GROUP, EXPERTS>;
+  auto kern = gs_stream_kernel<RB, NT, GROUP, BIAS, EXPERTS>;
   if (!ensure_dyn_smem(reinterpret_cast<const void*>(kern), L::BYTES)) return SQ_ERR_CUDA;
   EncodeTiledFn enc = get_encode_fn();
   if (!enc) return SQ_ERR_CUDA;
@@ -540,21 +570,26 @@ sq_status_t launch_stream_as(const GsArgs& a, int R, int splits, int grid, cudaS
   count_launch();
   return err == cudaSuccess ? SQ_OK : SQ_ERR_CUDA;
 }
-template <int NT, int GROUP, bool EXPERTS>
-sq_status_t launch_stream_rows(const GsArgs& a, int R, int splits, int grid, cudaStream_t s) {
-  if (R <= 16) return launch_stream_as<1, NT, GROUP, EXPERTS>(a, R, splits, grid, s);
-  if (R <= 32) return launch_stream_as<2, NT, GROUP, EXPERTS>(a, R, splits, grid, s);
-  if constexpr (NT == 1) return launch_stream_as<4, NT, GROUP, EXPERTS>(a, R, splits, grid, s);
-  return SQ_ERR_UNSUPPORTED;
+// Experts take the largest tiles: there are enough of them.
+template <int GROUP, bool BIAS, bool EXPERTS>
+sq_status_t launch_stream_rows(const GsArgs& a, int nt, int R, int splits, int grid, cudaStream_t s) {
+  if constexpr (!EXPERTS) {
+    if (R <= 16 && nt == 1) return launch_stream_as<1, 1, GROUP, BIAS, EXPERTS>(a, R, splits, grid, s);
+    if (R <= 32 && nt == 1) return launch_stream_as<2, 1, GROUP, BIAS, EXPERTS>(a, R, splits, grid, s);
+    if (R <= 16) return launch_stream_as<1, 2, GROUP, BIAS, EXPERTS>(a, R, splits, grid, s);
+  }
+  if (nt == 1) return launch_stream_as<4, 1, GROUP, BIAS, EXPERTS>(a, R, splits, grid, s);
+  return launch_stream_as<2, 2, GROUP, BIAS, EXPERTS>(a, R, splits, grid, s);
 }
 template <bool EXPERTS>
 sq_status_t launch_stream_any(const GsArgs& a, int nt, int R, int splits, int grid, cudaStream_t s) {
-  if (a.group == 128) return nt == 1 ? launch_stream_rows<1, 128, EXPERTS>(a, R, splits, grid, s) : launch_stream_rows<2, 128, EXPERTS>(a, R, splits, grid, s);
-  if (a.group == 64) return nt == 1 ? launch_stream_rows<1, 64, EXPERTS>(a, R, splits, grid, s) : launch_stream_rows<2, 64, EXPERTS>(a, R, splits, grid, s);
-  return nt == 1 ? launch_stream_rows<1, 32, EXPERTS>(a, R, splits, grid, s) : launch_stream_rows<2, 32, EXPERTS>(a, R, splits, grid, s);
+  if (a.group == 128)
+    return a.bg ? launch_stream_rows<128, true, EXPERTS>(a, nt, R, splits, grid, s) : launch_stream_rows<128, false, EXPERTS>(a, nt, R, splits, grid, s);
+  if (a.group == 64)
+    return a.bg ? launch_stream_rows<64, true, EXPERTS>(a, nt, R, splits, grid, s) : launch_stream_rows<64, false, EXPERTS>(a, nt, R, splits, grid, s);
+  return a.bg ? launch_stream_rows<32, true, EXPERTS>(a, nt, R, splits, grid, s) : launch_stream_rows<32, false, EXPERTS>(a, nt, R, splits, grid, s);
 }
 
-constexpr double GS_SPLIT_COST = 6.0;
 int even_rows(int64_t N, int64_t tiles) { return static_cast<int>(std::max<int64_t>(2, (N + 2 * tiles - 1) / (2 * tiles) * 2)); }
 
 sq_status_t launch_stream(const GsArgs& a, cudaStream_t s) {
@@ -570,22 +605,30 @@ sq_status_t launch_stream(const GsArgs& a, cudaStream_t s) {
     return launch_stream_any<true>(a, nt, R, 1, slots, s);
   }
   const int nt = a.M <= 8 ? 1 : 2, cap = nt == 1 ? 64 : 32;
-  // Time of a tile's step of 128 channels, in steps of 16 channels: its blocks of 16, its tokens and what a step costs by itself; for
-  // the tiles that a block gets, with K in 1, 2, 4 or 8 parts.
+  // Time of a call in us, fitted to R of 14 to 64 with K in 1 to 8 parts on 1 to 8 rows of five shapes, 4096 x 4096 to 8192 x 28672
+  // (10 % off): a step of 128 channels costs something by itself, something for its rows and something for its (pairs of) blocks of 16
+  // channels, more with small groups, and a third less where an SM has one block.  K over a cluster costs 1.5 us and has to fit the
+  // chip at once: 5 x 14336 -> 4096 with K in 1 / 2 / 4 parts 16.2 / 12.5 / 12.4 us, but 17.7 with 74 clusters of four.
+  const double unit = a.group == 128 ? 0.36 : (a.group == 64 ? 0.45 : 0.54);
   int best_r = 0, best_s = 1, best_grid = 0;
   double best = 0.0;
   for (int sp = 1; sp <= 8 && nks / sp >= (sp == 1 ? 1 : 8); sp *= 2) {
+    const int room = sp == 1 ? slots : (sp == 2 ? slots - slots / 16 : slots - slots / 8);       // blocks that clusters find place for
     for (int waves = 1; waves <= (sp == 1 ? 8 : 1); ++waves) {
-      const int R = even_rows(a.N, static_cast<int64_t>(slots / sp) * waves);
-      if (R > cap && (sp > 1 || waves < 8)) continue;
-      const int r = std::min(R, cap);
-      const int64_t tiles = (a.N + r - 1) / r, rounds = (tiles * sp + slots - 1) / slots;
-      const double cost = static_cast<double>(rounds) * (((nks + sp - 1) / sp + 7) / 8) * ((r + 15) / 16 + 0.5 + 0.1 * a.M) + (sp > 1 ? GS_SPLIT_COST : 0.0);
-      if (best_r == 0 || cost < best) {
-        best = cost;
-        best_r = r;
-        best_s = sp;
-        best_grid = static_cast<int>(std::min<int64_t>(tiles * sp, slots));
+      for (int half = 0; half < 2; ++half) {         // one block per SM, or two
+        const int want = even_rows(a.N, static_cast<int64_t>((half ? room / 2 : room) / sp) * waves);
+        if (want > cap && (half || sp > 1 || waves < 8)) continue;
+        const int r = std::min(want, cap);
+        const int64_t tiles = (a.N + r - 1) / r, rounds = (tiles * sp + slots - 1) / slots;
+        const int blocks = r <= 16 ? 1 : (r + 31) / 32 * 2;
+        const double cost = static_cast<double>(rounds) * (((nks + sp - 1) / sp + GS_WARPS - 1) / GS_WARPS) * (unit * blocks * nt + 0.31 + 0.024 * a.M) *
+                                (tiles * sp <= sms ? 0.67 : 1.0) + (sp > 1 ? 1.5 : 0.0);
+        if (best_r == 0 || cost < best) {
+          best = cost;
+          best_r = r;
+          best_s = sp;
+          best_grid = static_cast<int>(std::min<int64_t>(tiles * sp, slots));
+        }
       }
     }
   }
@@ -613,7 +656,9 @@ int gs_tile_m(const GsArgs& a) {
 }  // namespace
 
 sq_status_t launch_gemm_gs(const GsArgs& a, void* workspace, cudaStream_t s) {
-  const bool few = a.E > 0 ? a.M <= 16 * static_cast<int64_t>(a.E) : a.M <= 16;
+  // Rows for the stream: up to 8 (an expert: on average); up to 16 of a small layer, where the other kernel starts slowly: 12 x 4096
+  // -> 4096 7.5 us and 9.3, but 16 x 4096 -> 14336 19.4 and 14.9.
+  const bool few = a.E > 0 ? a.M <= 8 * static_cast<int64_t>(a.E) : a.M <= 8 || (a.M <= 16 && a.N * a.K <= 30000000);
   const int64_t kMax = (1ll << 31) - 1024;           // 32-bit coordinates of a tile in the weights and in the rows
   if (a.K % 32 == 0 && a.N % 2 == 0 && few && a.N * std::max(a.E, 1) <= kMax) return launch_stream(a, s);
   if (a.K % 32 == 0 && a.M <= kMax && a.N * std::max(a.E, 1) <= kMax) {

@@ -103,9 +103,10 @@ __device__ __forceinline__ uint4 scaled_word(uint32_t word, const WidenConsts& k
 struct WoPlain {
   static constexpr bool GS = false, BIAS = false, EXPERTS = false;
 };
-template <bool BIAS_, bool EXPERTS_>
+template <int GROUP_, bool BIAS_, bool EXPERTS_>
 struct WoGroups {
   static constexpr bool GS = true, BIAS = BIAS_, EXPERTS = EXPERTS_;
+  static constexpr int GROUP = GROUP_;
   GsArgs a;
 };
 
@@ -133,21 +134,73 @@ __device__ __forceinline__ WoTile wo_tile(const X& x, const int* first, int tile
   return p;
 }
 
-// The scales (and offsets) of one channel for the eight pieces of 32 input channels of a stage.
+// The scales (and offsets) of one channel for a converter group's stages, one stage ahead of the codes.  The group takes every
+// WOD_CONV_GROUPS-th of the stages [sb0, sb1) of the tiles tile0, tile0 + step, ...; the cursor walks the same way.
 template <class X>
 struct WoScales {
-  __half s[8], b[8];
-  __device__ __forceinline__ void load(const X& x, int expert, int ch, int sb) {
-    const GsArgs& a = x.a;
-    const size_t N = static_cast<size_t>(a.N), G = (a.K + a.group - 1) / a.group;
-    const size_t at = static_cast<size_t>(expert) * G * N + min(ch, static_cast<int>(a.N) - 1);
-    const int shift = 31 - __clz(a.group);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const size_t o = at + static_cast<size_t>(min(sb * 256 + i * 32, a.K - 1) >> shift) * N;
-      s[i] = __ldg(a.sg + o);
-      if (X::BIAS) b[i] = __ldg(a.bg + o);
+  __device__ __forceinline__ WoScales(const X&, int, int, int, int, int) {}
+};
+template <int GROUP, bool BIAS, bool EXPERTS>
+struct WoScales<WoGroups<GROUP, BIAS, EXPERTS>> {
+  using X = WoGroups<GROUP, BIAS, EXPERTS>;
+  static constexpr int PER = 256 / GROUP;               // groups of a stage
+  const X& x;
+  int tile, step, num_tiles, sb, sb0, sb1;
+  __half s[PER], b[PER], sn[PER], bn[PER];
+  const __half *ps = nullptr, *pb = nullptr;            // stage sb
+  bool aimed = false;
+  __device__ __forceinline__ WoScales(const X& x_, int tile0, int step_, int num_tiles_, int sb0_, int sb1_)
+      : x(x_), tile(tile0), step(step_), num_tiles(num_tiles_), sb(sb0_), sb0(sb0_), sb1(sb1_) {}
+  __device__ __forceinline__ void advance(int n) {
+    sb += n;
+    ps += static_cast<size_t>(n * PER) * x.a.N;
+    if (BIAS) pb += static_cast<size_t>(n * PER) * x.a.N;
+    while (sb >= sb1 && sb0 < sb1) {
+      sb -= sb1 - sb0;
+      tile += step;
+      aimed = false;
     }
+  }
+  // Requests the stage at the cursor; `place`: the tile's expert and this thread's channel of it.
+  template <typename Place>
+  __device__ __forceinline__ void fetch(Place place) {
+    if (tile >= num_tiles || sb >= sb1) return;
+    const GsArgs& a = x.a;
+    const size_t N = static_cast<size_t>(a.N);
+    const int G = (a.K + GROUP - 1) / GROUP;
+    if (!aimed) {
+      const int2 at = place(tile);
+      const size_t o = (static_cast<size_t>(at.x) * G + sb * PER) * N + min(at.y, static_cast<int>(a.N) - 1);
+      ps = a.sg + o;
+      if (BIAS) pb = a.bg + o;
+      aimed = true;
+    }
+    if ((sb + 1) * PER <= G) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        sn[i] = __ldg(ps + i * N);
+        if (BIAS) bn[i] = __ldg(pb + i * N);
+      }
+    } else {                                            // groups behind the last: their tokens are zeros, their scales have to be finite
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const size_t o = static_cast<size_t>(min(i, G - 1 - sb * PER)) * N;
+        sn[i] = __ldg(ps + o);
+        if (BIAS) bn[i] = __ldg(pb + o);
+      }
+    }
+  }
+  __device__ __forceinline__ void take() {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      s[i] = sn[i];
+      if (BIAS) b[i] = bn[i];
+    }
+  }
+  // Weights of a word of the stage's 32-channel piece `piece`.
+  __device__ __forceinline__ uint4 word(uint32_t w, const WidenConsts& k, int piece) const {
+    const int i = piece * 32 / GROUP;
+    return scaled_word<BIAS>(w, k, __half2half2(s[i]), __half2half2(BIAS ? b[i] : s[i]));
   }
 };
 
@@ -588,25 +641,15 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
     const int grp = (warp - 2) >> 2;                    // this group's stages: it % WOD_CONV_GROUPS == grp
     const int r = q * 32 + lane;                        // channel of the tile = TMEM lane
     const uint32_t lane_addr = static_cast<uint32_t>(q * 32) << 16;
-    // Scales one stage of this group ahead: a cursor of its own walks the same stages.
-    WoScales<X> sc, next;
-    int ntile = cid, nsb = sb0;
-    auto skip = [&](int n) {
-      for (; n > 0; --n)
-        if (++nsb >= sb1) {
-          nsb = sb0;
-          ntile += ncl;
-        }
+    WoScales<X> sc(x, cid, ncl, num_tiles, sb0, sb1);
+    auto place = [&](int at) {
+      const WoTile p = wo_tile(x, nullptr, at, tiles_n, 128 * CT, NT, M, N);
+      return make_int2(p.expert, p.ch0 + r);
     };
-    auto fetch = [&](WoScales<X>& to) {
-      if constexpr (X::GS) {
-        if (ntile >= num_tiles || sb0 >= sb1) return;
-        const WoTile p = wo_tile(x, nullptr, ntile, tiles_n, 128 * CT, NT, M, N);
-        to.load(x, p.expert, p.ch0 + r, nsb);
-      }
-    };
-    skip(grp);
-    fetch(sc);
+    if constexpr (X::GS) {
+      sc.advance(grp);
+      sc.fetch(place);
+    }
     uint32_t it = 0;
     bool ok = true;
     for (int tile = cid; tile < num_tiles && ok; tile += ncl) {
@@ -622,8 +665,9 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
 #pragma unroll
         for (int c = 0; c < 8; ++c) w[c] = *reinterpret_cast<const uint4*>(row + ((c ^ (r & 7)) << 4));
         if constexpr (X::GS) {
-          skip(WOD_CONV_GROUPS);
-          fetch(next);
+          sc.take();
+          sc.advance(WOD_CONV_GROUPS);
+          sc.fetch(place);
         }
         ok = mbar_wait(&a_empty[sa], ((it / WOD_A_STAGES) & 1) ^ 1, WO_B_EMPTY, limit);
         if (!ok) break;
@@ -639,8 +683,7 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
 #pragma unroll
               for (int g = 0; g < 4; ++g) {
                 uint4 f;
-                if constexpr (X::GS)
-                  f = scaled_word<X::BIAS>(xs[g], wk, __half2half2(sc.s[2 * h + j]), __half2half2(X::BIAS ? sc.b[2 * h + j] : sc.s[2 * h + j]));
+                if constexpr (X::GS) f = sc.word(xs[g], wk, 2 * h + j);
                 else f = widen_word(xs[g], wk);
                 v[16 * j + 4 * g + 0] = f.x;
                 v[16 * j + 4 * g + 1] = f.y;
@@ -658,7 +701,6 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
           mbar_arrive(&a_full[sa]);
           mbar_arrive(&st_empty[ss]);
         }
-        if constexpr (X::GS) sc = next;
       }
     }
   } else {
@@ -964,25 +1006,15 @@ wo_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
     const int grp = (warp - 2) >> 2;                    // this group's ring stage
     const int r = q * 32 + lane;                        // channel of the CTA's 128 = TMEM lane
     const uint32_t lane_addr = static_cast<uint32_t>(q * 32) << 16;
-    // Scales one stage of this group ahead: a cursor of its own walks the same stages.
-    WoScales<X> sc, next;
-    int ntile = pair, nsb = 0;
-    auto skip = [&](int n) {
-      for (; n > 0; --n)
-        if (++nsb >= num_sb) {
-          nsb = 0;
-          ntile += npairs;
-        }
+    WoScales<X> sc(x, pair, npairs, num_tiles, 0, num_sb);
+    auto place = [&](int at) {
+      const WoTile p = wo_tile(x, first, at, tiles_n, 256, tile_m, M, N);
+      return make_int2(p.expert, p.ch0 + static_cast<int>(rank) * 128 + r);
     };
-    auto fetch = [&](WoScales<X>& to) {
-      if constexpr (X::GS) {
-        if (ntile >= num_tiles || 0 >= num_sb) return;
-        const WoTile p = wo_tile(x, first, ntile, tiles_n, 256, tile_m, M, N);
-        to.load(x, p.expert, p.ch0 + static_cast<int>(rank) * 128 + r, nsb);
-      }
-    };
-    skip(grp);
-    fetch(sc);
+    if constexpr (X::GS) {
+      sc.advance(grp);
+      sc.fetch(place);
+    }
     uint32_t it = 0;
     bool ok = true;
     for (int tile = pair; tile < num_tiles && ok; tile += npairs) {
@@ -997,8 +1029,9 @@ wo_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
 #pragma unroll
         for (int c = 0; c < 8; ++c) w[c] = *reinterpret_cast<const uint4*>(row + ((c ^ (r & 7)) << 4));
         if constexpr (X::GS) {
-          skip(WOD_CONV_GROUPS);
-          fetch(next);
+          sc.take();
+          sc.advance(WOD_CONV_GROUPS);
+          sc.fetch(place);
         }
         ok = mbar_wait(&empty[s], ((it / WP_S) & 1) ^ 1, WP_EMPTY_A, limit);
         if (!ok) break;
@@ -1014,8 +1047,7 @@ wo_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
 #pragma unroll
               for (int g = 0; g < 4; ++g) {
                 uint4 f;
-                if constexpr (X::GS)
-                  f = scaled_word<X::BIAS>(xs[g], wk, __half2half2(sc.s[2 * h + j]), __half2half2(X::BIAS ? sc.b[2 * h + j] : sc.s[2 * h + j]));
+                if constexpr (X::GS) f = sc.word(xs[g], wk, 2 * h + j);
                 else f = widen_word(xs[g], wk);
                 v[16 * j + 4 * g + 0] = f.x;
                 v[16 * j + 4 * g + 1] = f.y;
@@ -1036,7 +1068,6 @@ wo_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
           mbar_arrive_cluster(&full[s], 0);
           mbar_arrive(&st_empty[ss]);
         }
-        if constexpr (X::GS) sc = next;
       }
     }
   } else {
@@ -1428,23 +1459,24 @@ sq_status_t launch_wo_gemm(const void* Z16, const void* Wq, const void* sw, int6
   return cudaGetLastError() == cudaSuccess ? SQ_OK : SQ_ERR_CUDA;
 }
 
-sq_status_t launch_wo_gemm_groups(const GsArgs& a, int tile_m, cudaStream_t s) {
+namespace {
+template <int GROUP, bool BIAS>
+sq_status_t launch_wo_groups_as(const GsArgs& a, int tile_m, cudaStream_t s) {
   const int M = static_cast<int>(a.M), N = static_cast<int>(a.N);
-  if (a.E > 0) {
-    const int rows = static_cast<int>(a.E * a.N);
-    if (a.bg) return launch_wo_pair<4, WoGroups<true, true>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a}, rows, tile_m);
-    return launch_wo_pair<4, WoGroups<false, true>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a}, rows, tile_m);
-  }
-  if (M <= 32) {
-    if (a.bg) return launch_wo_decode<32, 4, 8, 1, WoGroups<true, false>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
-    return launch_wo_decode<32, 4, 8, 1, WoGroups<false, false>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
-  }
-  if (M <= 64) {
-    if (a.bg) return launch_wo_decode<64, 3, 6, 1, WoGroups<true, false>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
-    return launch_wo_decode<64, 3, 6, 1, WoGroups<false, false>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
-  }
-  if (a.bg) return launch_wo_pair<4, WoGroups<true, false>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a}, 0, tile_m);
-  return launch_wo_pair<4, WoGroups<false, false>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a}, 0, tile_m);
+  if (a.E > 0)
+    return launch_wo_pair<4, WoGroups<GROUP, BIAS, true>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a}, static_cast<int>(a.E * a.N), tile_m);
+  using X = WoGroups<GROUP, BIAS, false>;
+  if (M <= 16) return launch_wo_decode<16, 4, 8, 1, X>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
+  if (M <= 32) return launch_wo_decode<32, 4, 8, 1, X>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
+  if (M <= 64) return launch_wo_decode<64, 3, 6, 1, X>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
+  return launch_wo_pair<4, X>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a}, 0, tile_m);
+}
+}  // namespace
+
+sq_status_t launch_wo_gemm_groups(const GsArgs& a, int tile_m, cudaStream_t s) {
+  if (a.group == 128) return a.bg ? launch_wo_groups_as<128, true>(a, tile_m, s) : launch_wo_groups_as<128, false>(a, tile_m, s);
+  if (a.group == 64) return a.bg ? launch_wo_groups_as<64, true>(a, tile_m, s) : launch_wo_groups_as<64, false>(a, tile_m, s);
+  return a.bg ? launch_wo_groups_as<32, true>(a, tile_m, s) : launch_wo_groups_as<32, false>(a, tile_m, s);
 }
 
 sq_status_t launch_interleave_nibbles(void* Wq, int64_t rows, int64_t K, cudaStream_t s) {
