@@ -462,19 +462,20 @@ struct WoDecSmem {
   static constexpr int DYN_BYTES = TOTAL + 1024;
 };
 
-template <int NT, int ST, int SS, int CT, class X>
-__global__ void __launch_bounds__(WOD_THREADS, 1)
+template <int NT, int ST, int SS, int CT, int CG, class X>
+__global__ void __launch_bounds__((3 + 4 * CG + WO_EPI_WARPS) * 32, 1)
 wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_constant__ CUtensorMap tmap_w,
                       const __half* __restrict__ sw, int M, int N, int K, __half* __restrict__ Y, int splits,
                       const __grid_constant__ X x) {
   using L = WoDecSmem<NT, ST, SS>;
+  constexpr int T_WARP = 2 + 4 * CG + WO_EPI_WARPS;      // the token loads have a warp of their own
   // CT = channel tiles of 128 that share a token tile (1 or 2).  With one, two accumulators alternate
   // between tiles (the epilogue of a tile runs under the next tile's MMAs); with two, both accumulators
   // belong to the same tile -- channels [0, 128) and [128, 256) of it -- and every token block that
   // reaches shared memory feeds two MMAs instead of one.
   static_assert(CT == 1 || CT == 2, "one or two channel tiles per token tile");
-  static_assert(2 * NT + 128 * WOD_A_STAGES <= 512, "tensor-memory plan does not fit");
-  static_assert(SS % WOD_CONV_GROUPS == 0 && WOD_A_STAGES % WOD_CONV_GROUPS == 0, "a converter group meets every phase of its stages");
+  static_assert(2 * NT + 128 * CG <= 512, "tensor-memory plan does not fit");
+  static_assert(SS % CG == 0, "a converter group meets every phase of its stages");
   constexpr int NBUF = 2 / CT;                           // accumulator sets that alternate between tiles
   constexpr int WOD_A_COL0 = 2 * NT > 128 ? 2 * NT : 128;
   griddep_launch_dependents();
@@ -485,9 +486,10 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
   uint64_t* t_empty = t_full + ST;
   uint64_t* st_full = t_empty + ST;
   uint64_t* st_empty = st_full + SS;
-  uint64_t* a_full = st_empty + SS;
-  uint64_t* a_empty = a_full + WOD_A_STAGES;
-  uint64_t* tmem_full = a_empty + WOD_A_STAGES;   // [2]
+  __shared__ uint64_t a_bars[2 * CG];             // (the plan has room for two stages)
+  uint64_t* a_full = a_bars;
+  uint64_t* a_empty = a_full + CG;
+  uint64_t* tmem_full = st_empty + SS;            // [2]
   uint64_t* tmem_empty = tmem_full + 2;           // [2]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_TMEM);
 
@@ -535,7 +537,7 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
       mbar_init(&t_empty[s], 1);
     }
     for (int s = 0; s < SS; ++s) mbar_init(&st_empty[s], 4);          // the four warps of one converter group
-    for (int s = 0; s < WOD_A_STAGES; ++s) {
+    for (int s = 0; s < CG; ++s) {
       mbar_init(&a_full[s], 4);
       mbar_init(&a_empty[s], 1);
     }
@@ -571,7 +573,7 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
         }
       }
     }
-  } else if (warp == WOD_T_WARP) {
+  } else if (warp == T_WARP) {
     // ------------------------------ token loads: a block serves all channel tiles of its token tile -------
     griddep_wait();                                     // Z16 may come from the kernel launched before this one
     if (lane == 0) {
@@ -608,10 +610,10 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
 #pragma unroll
           for (int half = 0; half < CT; ++half, ++it) {
             const uint32_t tit = it / CT;
-            const int st = tit % ST, sa = it % WOD_A_STAGES;
+            const int st = tit % ST, sa = it % CG;
             const int nk = (num_kb - 4 * sb) < 4 ? (num_kb - 4 * sb) : 4;
             if (half == 0) ok = mbar_wait(&t_full[st], (tit / ST) & 1, WO_A_FULL, limit);
-            ok = ok && mbar_wait(&a_full[sa], (it / WOD_A_STAGES) & 1, WO_B_FULL, limit);
+            ok = ok && mbar_wait(&a_full[sa], (it / CG) & 1, WO_B_FULL, limit);
             if (!ok) break;
             tc_fence_after_sync();
             const uint32_t tmem_d = tmem_base + (b * CT + half) * NT;
@@ -634,11 +636,11 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
         umma_commit(&tmem_full[b]);
       }
     }
-  } else if (warp < 2 + WOD_CONV_WARPS) {
+  } else if (warp < 2 + 4 * CG) {
     // ------------------------------ weight converters: staging -> registers -> tensor memory ------
     const WidenConsts wk = widen_consts();
     const int q = warp & 3;
-    const int grp = (warp - 2) >> 2;                    // this group's stages: it % WOD_CONV_GROUPS == grp
+    const int grp = (warp - 2) >> 2;                    // this group's stages: it % CG == grp
     const int r = q * 32 + lane;                        // channel of the tile = TMEM lane
     const uint32_t lane_addr = static_cast<uint32_t>(q * 32) << 16;
     WoScales<X> sc(x, cid, ncl, num_tiles, sb0, sb1);
@@ -654,9 +656,9 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
     bool ok = true;
     for (int tile = cid; tile < num_tiles && ok; tile += ncl) {
       for (int sbh = sb0 * CT; sbh < sb1 * CT && ok; ++sbh, ++it) {
-        if ((it % WOD_CONV_GROUPS) != static_cast<uint32_t>(grp)) continue;
+        if ((it % CG) != static_cast<uint32_t>(grp)) continue;
         const int sb = sbh / CT;
-        const int ss = it % SS, sa = it % WOD_A_STAGES;
+        const int ss = it % SS, sa = it % CG;
         const int nk = (num_kb - 4 * sb) < 4 ? (num_kb - 4 * sb) : 4;
         ok = mbar_wait(&st_full[ss], (it / SS) & 1, WO_ST_FULL, limit);
         if (!ok) break;
@@ -666,10 +668,10 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
         for (int c = 0; c < 8; ++c) w[c] = *reinterpret_cast<const uint4*>(row + ((c ^ (r & 7)) << 4));
         if constexpr (X::GS) {
           sc.take();
-          sc.advance(WOD_CONV_GROUPS);
+          sc.advance(CG);
           sc.fetch(place);
         }
-        ok = mbar_wait(&a_empty[sa], ((it / WOD_A_STAGES) & 1) ^ 1, WO_B_EMPTY, limit);
+        ok = mbar_wait(&a_empty[sa], ((it / CG) & 1) ^ 1, WO_B_EMPTY, limit);
         if (!ok) break;
         tc_fence_after_sync();
 #pragma unroll
@@ -768,7 +770,7 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
     // Every thread of every CTA of the cluster comes through here, whatever happened above: the two
     // barriers are hardware barriers, not polled waits.
     cluster_sync_all();                                 // the partial tiles are in place
-    if (crank == 0 && warp >= 2 + WOD_CONV_WARPS && warp < WOD_T_WARP && cid < num_tiles) {
+    if (crank == 0 && warp >= 2 + 4 * CG && warp < T_WARP && cid < num_tiles) {
       tc_fence_after_sync();
       const int quarter = warp & 3;
       const int ch = (cid % tiles_n) * 128 + quarter * 32 + lane;                          // CT = 1 here
@@ -1320,7 +1322,10 @@ sq_status_t launch_wo_decode(const void* Z16, const void* Wq, const void* sw, in
           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return SQ_ERR_CUDA;
   if (!make_packed_map(&mw, Wq, N, K / 2, 128)) return SQ_ERR_CUDA;
-  auto kern = wo_gemm_tmem_kernel<NT, ST, SS, CT, X>;
+  // Group scales make the converters' work longer: a third group of them, with an operand stage of its own (50 x 8192 -> 28672
+  // 51.8 -> 45.4 us).
+  constexpr int CG = X::GS ? 3 : WOD_CONV_GROUPS;
+  auto kern = wo_gemm_tmem_kernel<NT, ST, SS, CT, CG, X>;
   if (!ensure_dyn_smem(reinterpret_cast<const void*>(kern), L::DYN_BYTES)) return SQ_ERR_CUDA;
   const int sms = sm_count();
   if (sms <= 0) return SQ_ERR_CUDA;
@@ -1331,7 +1336,7 @@ sq_status_t launch_wo_decode(const void* Z16, const void* Wq, const void* sw, in
   int splits = 1;
   while (CT == 1 && splits < 4 && tiles * splits * 2 <= sms && num_sb / (splits * 2) >= 4) splits *= 2;
   const int grid = splits > 1 ? tiles * splits : (tiles < sms ? tiles : sms);
-  const cudaError_t err = launch_cluster_maybe_pdl(kern, dim3(grid), dim3(WOD_THREADS), L::DYN_BYTES, s,
+  const cudaError_t err = launch_cluster_maybe_pdl(kern, dim3(grid), dim3((3 + 4 * CG + WO_EPI_WARPS) * 32), L::DYN_BYTES, s,
                                                    static_cast<unsigned>(splits), mz, mw, static_cast<const __half*>(sw),
                                                    M, N, K, static_cast<__half*>(Y), splits, x);
   count_launch();
@@ -1466,8 +1471,8 @@ sq_status_t launch_wo_groups_as(const GsArgs& a, int tile_m, cudaStream_t s) {
   if (a.E > 0)
     return launch_wo_pair<4, WoGroups<GROUP, BIAS, true>>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a}, static_cast<int>(a.E * a.N), tile_m);
   using X = WoGroups<GROUP, BIAS, false>;
-  if (M <= 16) return launch_wo_decode<16, 4, 8, 1, X>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
-  if (M <= 32) return launch_wo_decode<32, 4, 8, 1, X>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
+  if (M <= 16) return launch_wo_decode<16, 4, 9, 1, X>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
+  if (M <= 32) return launch_wo_decode<32, 4, 9, 1, X>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
   if (M <= 64) return launch_wo_decode<64, 3, 6, 1, X>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a});
   return launch_wo_pair<4, X>(a.Z, a.Wq, nullptr, M, N, a.K, a.Y, s, {a}, 0, tile_m);
 }

@@ -26,8 +26,9 @@
 namespace sq {
 namespace {
 
-constexpr int RT_THREADS = 512;
-constexpr int RT_MAX_BLOCKS = 148;                   // the second kernel reads every block's counts
+constexpr int RT_MAX_BLOCKS = 148;                   // the second kernel reads every block's counts, five to a lane
+constexpr int RT_STAGED = 4096;                      // slots of a block whose expert and rank stay in shared memory
+constexpr int RT_CHUNKS = 4;                         // blocks of the first kernel that one of the second finishes
 constexpr uint32_t RT_KEY_NINF = 0x007FFFFFu;        // route_key(-inf): not above it is not usable
 constexpr float RT_NINF = -__builtin_huge_valf();
 
@@ -86,6 +87,10 @@ __device__ __forceinline__ void route_load(const RouteArgs& a, long long t, int 
         x[2 * j] = mine ? bits_to_float(w[j & 1] & 0xFFFFu, a.dtype) : RT_NINF;
         x[2 * j + 1] = mine ? bits_to_float(w[j & 1] >> 16, a.dtype) : RT_NINF;
       }
+    } else if (EPL == 2 && a.vec) {
+      const uint32_t v = mine ? *reinterpret_cast<const uint32_t*>(row) : 0u;
+      x[0] = mine ? bits_to_float(v & 0xFFFFu, a.dtype) : RT_NINF;
+      x[EPL - 1] = mine ? bits_to_float(v >> 16, a.dtype) : RT_NINF;
     } else {
 #pragma unroll
       for (int i = 0; i < EPL; ++i) x[i] = e0 + i < a.E ? bits_to_float(row[i], a.dtype) : RT_NINF;
@@ -100,8 +105,10 @@ __device__ __forceinline__ uint32_t route_key(float x) {
   const uint32_t u = __float_as_uint(x + 0.0f);
   return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
 }
-// exp(x - m) for x <= m: 1 at x == m, infinite or not.
-__device__ __forceinline__ float route_exp(float x, float m) { return x == m ? 1.0f : expf(x - m); }
+// exp(x - m) for x <= m: 1 at x == m, infinite or not.  (__expf: 2 + 1.2 |x - m| ulp, as much as rounding x - m costs.)
+__device__ __forceinline__ float route_exp(float x, float m) { return x == m ? 1.0f : __expf(x - m); }
+// Logits of 16 bits and their place in one key: larger logits first, then lower places, and no two alike.
+__device__ __forceinline__ uint32_t route_key16(float x, int e) { return (route_key(x) & 0xFFFFE000u) | static_cast<uint32_t>(0x1FFF - e); }
 
 template <int LPT>
 __device__ __forceinline__ float group_max(float v) {
@@ -137,19 +144,6 @@ __device__ __forceinline__ bool route_softmax(const float (&x)[EPL], float (&p)[
   return usable;
 }
 
-// What one block of the second kernel, or the only block of the first, does with the counts of all blocks before it.
-__device__ __forceinline__ void route_place(const int* base, const int32_t* ids, int32_t* pos, int32_t* row_token, long long first,
-                                            long long last, int k) {
-  for (long long i = first * k + threadIdx.x; i < last * k; i += blockDim.x) {
-    const int id = ids[i];
-    if (id >= 0) {
-      const int r = pos[i] + base[id];
-      pos[i] = r;
-      row_token[r] = static_cast<int32_t>(i / k);
-    }
-  }
-}
-
 __device__ __forceinline__ double block_sum(double v, double* sums) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
@@ -162,25 +156,84 @@ __device__ __forceinline__ double block_sum(double v, double* sums) {
   return v;
 }
 
-// Shared memory: counters [groups][E] (int), base [E] (int) and, over the counters once they have been read, sums of p.
-template <int LPT, int EPL>
-__global__ void __launch_bounds__(RT_THREADS)
-route_kernel(const RouteArgs a, long long chunk, int32_t* __restrict__ ids, float* __restrict__ gates, int32_t* pos,
+// The k largest of the group's logits: lane j < k gets the j-th's expert (-1: none left) and value.  All lanes of the warp.
+// KEY16: the logits have 16 bits, so that one 32-bit maximum finds the logit and its expert; else the lowest of the lanes that
+// hold the maximum wins, and in it the lowest place.
+template <int LPT, int EPL, bool KEY16>
+__device__ __forceinline__ void route_select(const float (&x)[EPL], int sub, int k, int& my_id, float& my_x) {
+  uint32_t key[EPL];
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) key[i] = KEY16 ? route_key16(x[i], sub * EPL + i) : route_key(x[i]);
+  uint32_t mine = 0;
+  int where = 0;
+  for (int j = 0; j < k; ++j) {
+    uint32_t best = key[0];
+#pragma unroll
+    for (int i = 1; i < EPL; ++i) best = max(best, key[i]);
+    uint32_t top = best;
+    if (LPT == 32) {
+      top = __reduce_max_sync(0xFFFFFFFFu, best);
+    } else {
+#pragma unroll
+      for (int o = LPT / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    }
+    if (KEY16) {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) key[i] = key[i] == top ? 0u : key[i];
+      if (sub == j) mine = top;
+    } else {
+      const uint32_t who = __ballot_sync(0xFFFFFFFFu, best == top) >> (LPT == 32 ? 0 : (threadIdx.x & 31 & ~(LPT - 1)));
+      const int winner = __ffs(who & (LPT == 32 ? 0xFFFFFFFFu : (1u << (LPT & 31)) - 1u)) - 1;
+      bool open = sub == winner;
+      int at = 0;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) {
+        const bool hit = open && key[i] == top;
+        if (hit) { key[i] = 0; at = i; }
+        open = open && !hit;
+      }
+      at = __shfl_sync(0xFFFFFFFFu, at, winner, LPT);
+      if (sub == j) {
+        mine = top;
+        where = winner * EPL + at;
+      }
+    }
+  }
+  if (KEY16) {
+    where = 0x1FFF - static_cast<int>(mine & 0x1FFFu);
+    mine &= 0xFFFFE000u;
+    const bool usable = mine > (RT_KEY_NINF & 0xFFFFE000u);
+    my_id = usable ? where : -1;
+  } else {
+    my_id = mine > RT_KEY_NINF ? where : -1;
+  }
+  my_x = __uint_as_float(mine & 0x80000000u ? mine ^ 0x80000000u : ~mine & (KEY16 ? 0xFFFFE000u : 0xFFFFFFFFu));
+}
+
+// Shared memory: counters [groups][E], sums of p [groups][E], base [E], partial sums over groups [2][threads], and the block's slots
+// as (expert, rank) where they fit (staged).
+template <int LPT, int EPL, int THREADS, bool KEY16>
+__global__ void __launch_bounds__(THREADS)
+route_kernel(const RouteArgs a, long long chunk, int staged, int32_t* __restrict__ ids, float* __restrict__ gates, int32_t* pos,
              int32_t* __restrict__ hist, float* __restrict__ psum, int32_t* __restrict__ counts, int32_t* __restrict__ offsets,
              int32_t* __restrict__ row_token, float* __restrict__ loss) {
-  constexpr int GROUPS = RT_THREADS / LPT;
+  constexpr int GROUPS = THREADS / LPT;
   griddep_launch_dependents();
   extern __shared__ __align__(16) unsigned char rt_smem[];
-  int* cnt = reinterpret_cast<int*>(rt_smem);        // [GROUPS][E]
-  float* ps = reinterpret_cast<float*>(rt_smem) + static_cast<size_t>(GROUPS) * a.E;      // [GROUPS][E]
-  int* base = reinterpret_cast<int*>(ps + static_cast<size_t>(GROUPS) * a.E);             // [E]
+  const int E = a.E, k = a.k;
+  int* cnt = reinterpret_cast<int*>(rt_smem);                            // [GROUPS][E]
+  float* ps = reinterpret_cast<float*>(cnt + GROUPS * E);                // [GROUPS][E]
+  int* base = reinterpret_cast<int*>(ps + GROUPS * E);                   // [E]
+  int* part_c = base + E;                                                // [THREADS]
+  float* part_p = reinterpret_cast<float*>(part_c + THREADS);            // [THREADS]
+  int* slot_id = reinterpret_cast<int*>(part_p + THREADS);               // [RT_STAGED], [RT_STAGED]
+  int* slot_rank = slot_id + RT_STAGED;
   __shared__ int warp_sums[33];
   __shared__ double sums[32];
   __shared__ int live_of[GROUPS];
 
-  const int grp = threadIdx.x / LPT, sub = threadIdx.x % LPT, lane = threadIdx.x & 31;
-  const int E = a.E, k = a.k;
-  for (int i = threadIdx.x; i < GROUPS * E; i += RT_THREADS) cnt[i] = 0;
+  const int grp = threadIdx.x / LPT, sub = threadIdx.x % LPT;
+  for (int i = threadIdx.x; i < GROUPS * E; i += THREADS) cnt[i] = 0;
   __syncthreads();
   griddep_wait();                                    // the logits come from, and the outputs may be read by, the kernel before
 
@@ -189,78 +242,46 @@ route_kernel(const RouteArgs a, long long chunk, int32_t* __restrict__ ids, floa
   const long long t0 = first + grp * run, t1 = t0 + run < last ? t0 + run : last;
   int* my_cnt = cnt + grp * E;
   float acc[EPL], x[EPL], next[EPL];
+  bool next_live = false;
 #pragma unroll
   for (int i = 0; i < EPL; ++i) { acc[i] = 0.0f; next[i] = RT_NINF; }
   int live = 0;
-  if (t0 < t1) route_load<LPT, EPL>(a, t0, sub, next);
+  auto load = [&](long long t) {
+    route_load<LPT, EPL>(a, t, sub, next);
+    next_live = a.mask == nullptr || a.mask[t] != 0;
+  };
+  if (t0 < t1) load(t0);
   for (long long it = 0; it < run; ++it) {           // every group of a warp: the shuffles below are the warp's
     const long long t = t0 + it;
     const bool in = t < t1;
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) x[i] = in ? next[i] : RT_NINF;
-    if (t + 1 < t1) route_load<LPT, EPL>(a, t + 1, sub, next);
-    if (in && a.mask != nullptr && a.mask[t] == 0) {
-#pragma unroll
-      for (int i = 0; i < EPL; ++i) x[i] = RT_NINF;
-    }
+    for (int i = 0; i < EPL; ++i) x[i] = in && next_live ? next[i] : RT_NINF;
+    if (t + 1 < t1) load(t + 1);
     float p[EPL], m, inv;
     live += route_softmax<LPT, EPL>(x, p, m, inv) ? 1 : 0;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) acc[i] += p[i];
-
-    // The k largest: the lane's own best first, then the best of the lanes; equal ones to the lowest index.
-    uint32_t key[EPL], best = 0;
-    int bi = 0;
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      key[i] = route_key(x[i]);
-      if (key[i] > best) { best = key[i]; bi = i; }
-    }
-    int my_id = -1;
-    float my_e = 0.0f, ssel = 0.0f;
-    for (int j = 0; j < k; ++j) {
-      uint32_t top;
-      int winner;
-      if (LPT == 32) {
-        top = __reduce_max_sync(0xFFFFFFFFu, best);
-        winner = __ffs(__ballot_sync(0xFFFFFFFFu, best == top)) - 1;
-      } else {
-        top = best;
-#pragma unroll
-        for (int o = LPT / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        const uint32_t who = __ballot_sync(0xFFFFFFFFu, best == top) >> (lane & ~(LPT - 1) & 31);
-        winner = __ffs(who & (LPT == 32 ? 0xFFFFFFFFu : (1u << (LPT & 31)) - 1u)) - 1;
-      }
-      const int wi = __shfl_sync(0xFFFFFFFFu, bi, winner, LPT);
-      const bool usable = top > RT_KEY_NINF;
-      const float v = __uint_as_float(top & 0x80000000u ? top ^ 0x80000000u : ~top);      // the logit itself
-      const float ev = usable ? route_exp(v, m) : 0.0f;
-      ssel += ev;
-      if (sub == j) {
-        my_id = usable ? winner * EPL + wi : -1;
-        my_e = ev;
-      }
-      if (sub == winner) {
-        best = 0;
-        int nb = 0;
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) {
-          if (i == bi) key[i] = 0;
-          if (key[i] > best) { best = key[i]; nb = i; }
-        }
-        bi = nb;
-      }
-    }
+    int my_id;
+    float my_x;
+    route_select<LPT, EPL, KEY16>(x, sub, k, my_id, my_x);
+    if (sub >= k) my_id = -1;
+    const float ev = my_id >= 0 ? route_exp(my_x, m) : 0.0f;
+    const float scale = a.renorm ? 1.0f / group_sum<LPT>(ev) : inv;
     if (in && sub < k) {
       const long long o = t * k + sub;
       ids[o] = my_id;
-      gates[o] = my_id >= 0 ? (a.renorm ? my_e / ssel : my_e * inv) : 0.0f;
+      gates[o] = my_id >= 0 ? ev * scale : 0.0f;
       int r = -1;
       if (my_id >= 0) {                              // the token's experts differ: no two lanes share a counter
         r = my_cnt[my_id];
         my_cnt[my_id] = r + 1;
       }
-      pos[o] = r;                                    // within the group, for now
+      if (staged) {
+        slot_id[o - first * k] = my_id;
+        slot_rank[o - first * k] = r;
+      } else {
+        pos[o] = r;                                  // within the group, for now
+      }
     }
     __syncwarp();
   }
@@ -270,39 +291,64 @@ route_kernel(const RouteArgs a, long long chunk, int32_t* __restrict__ ids, floa
   if (sub == 0) live_of[grp] = live;
   __syncthreads();
 
-  // Counts of the groups before, and the block's own.
+  // Counts of the groups before, and the block's own: a thread takes an expert and one of `parts` runs of groups.
   const bool only = gridDim.x == 1;
+  const int parts = max(1, min(THREADS / E, 16)), per = (GROUPS + parts - 1) / parts;
   double part = 0.0;
   int n = 0;
-  for (int g = 0; g < GROUPS; ++g) n += live_of[g];
+  if (threadIdx.x < 32) {
+    for (int g = threadIdx.x; g < GROUPS; g += 32) n += live_of[g];
+    n = __reduce_add_sync(0xFFFFFFFFu, n);
+  }
   int carry = 0;
-  for (int e0 = 0; e0 < E; e0 += RT_THREADS) {       // (uniform: block_scan is the whole block's)
-    const int e = e0 + threadIdx.x;
+  for (int e0 = 0; e0 < E; e0 += THREADS / parts) {  // (uniform: the barriers are the whole block's; one round where E <= THREADS)
+    const int width = min(E - e0, THREADS / parts);
+    const int q = threadIdx.x / width, e = e0 + threadIdx.x % width;
+    const bool on = q < parts;
     int c = 0;
     float s = 0.0f;
-    if (e < E) {
-      for (int g = 0; g < GROUPS; ++g) {
-        const int v = cnt[g * E + e];
-        cnt[g * E + e] = c;
-        c += v;
+    if (on) {
+#pragma unroll 4
+      for (int g = q * per; g < min(GROUPS, (q + 1) * per); ++g) {
+        c += cnt[g * E + e];
         s += ps[g * E + e];
       }
-      if (!only) {
-        hist[static_cast<size_t>(blockIdx.x) * (E + 1) + e] = c;
-        psum[static_cast<size_t>(blockIdx.x) * E + e] = s;
-        base[e] = 0;
+      part_c[q * width + e - e0] = c;
+      part_p[q * width + e - e0] = s;
+    }
+    __syncthreads();
+    int before = 0, total = 0;
+    float psum_e = 0.0f;
+    if (on) {
+      for (int r = 0; r < parts; ++r) {
+        const int v = part_c[r * width + e - e0];
+        before += r < q ? v : 0;
+        total += v;
+        psum_e += part_p[r * width + e - e0];
+      }
+#pragma unroll 4
+      for (int g = q * per; g < min(GROUPS, (q + 1) * per); ++g) {
+        const int v = cnt[g * E + e];
+        cnt[g * E + e] = before;
+        before += v;
       }
     }
+    const bool mine = on && q == 0;
     if (only) {
-      const int off = carry + block_scan(c, warp_sums);
+      const int off = carry + block_scan(mine ? total : 0, warp_sums);
       carry += warp_sums[32];
-      if (e < E) {
+      if (mine) {
         base[e] = off;
-        counts[e] = c;
+        counts[e] = total;
         offsets[e] = off;
-        part += static_cast<double>(c) * s;
+        part += static_cast<double>(total) * psum_e;
       }
+    } else if (mine) {
+      hist[static_cast<size_t>(e) * gridDim.x + blockIdx.x] = total;
+      psum[static_cast<size_t>(e) * gridDim.x + blockIdx.x] = psum_e;
+      base[e] = 0;
     }
+    __syncthreads();
   }
   if (only) {
     const double all = block_sum(part, sums);
@@ -312,96 +358,108 @@ route_kernel(const RouteArgs a, long long chunk, int32_t* __restrict__ ids, floa
       if (loss != nullptr) *loss = n > 0 ? static_cast<float>(all * E / (static_cast<double>(k) * n * n)) : 0.0f;
     }
   } else if (threadIdx.x == 0) {
-    hist[static_cast<size_t>(blockIdx.x) * (E + 1) + E] = n;
+    hist[static_cast<size_t>(E) * gridDim.x + blockIdx.x] = n;
   }
-  __syncthreads();
   // The slots' rows within the block (or for good, and then the rows' tokens too).
   for (long long i = t0 * k + sub; i < t1 * k; i += LPT) {
-    const int id = ids[i];
+    const int id = staged ? slot_id[i - first * k] : ids[i];
+    int r = -1;
     if (id >= 0) {
-      const int r = pos[i] + cnt[grp * E + id] + base[id];
-      pos[i] = r;
+      r = (staged ? slot_rank[i - first * k] : pos[i]) + cnt[grp * E + id] + base[id];
       if (only) row_token[r] = static_cast<int32_t>(i / k);
     }
+    pos[i] = r;
   }
 }
 
-// Blocks 0 .. B-1: the final rows of block b's tokens.  Block B: counts, offsets and the loss.
+// Blocks 0 .. gridDim.x - 2: the final rows of RT_CHUNKS blocks' tokens.  The last block: counts, offsets and the loss.
+// Shared memory: base [RT_CHUNKS][E], total [E], sum of p [E].
 __global__ void __launch_bounds__(1024)
 route_finish_kernel(int B, int E, int k, long long T, long long chunk, const int32_t* __restrict__ hist,
                     const float* __restrict__ psum, const int32_t* __restrict__ ids, int32_t* pos, int32_t* __restrict__ counts,
                     int32_t* __restrict__ offsets, int32_t* __restrict__ row_token, float* __restrict__ loss) {
   griddep_launch_dependents();
   extern __shared__ __align__(16) unsigned char rt_smem[];
-  int* before = reinterpret_cast<int*>(rt_smem);     // [parts][E]: counts of the blocks before this one
-  const int parts = max(1, 1024 / E);
-  int* total = before + parts * E;                   // [parts][E]
-  float* prob = reinterpret_cast<float*>(total + parts * E);      // [parts][E], the last block's
+  int* base = reinterpret_cast<int*>(rt_smem);
+  int* total = base + RT_CHUNKS * E;
+  float* prob = reinterpret_cast<float*>(total + E);
   __shared__ int warp_sums[33];
   __shared__ double sums[32];
   griddep_wait();
 
-  const int b = blockIdx.x;
-  for (int i = threadIdx.x; i < parts * E; i += blockDim.x) {
-    const int e = i % E, part = i / E;
-    int s = 0, all = 0;
-    float q = 0.0f;
-    const int lo = part * B / parts, hi = (part + 1) * B / parts;
-#pragma unroll 8
-    for (int o = lo; o < hi; ++o) {
-      const int v = hist[static_cast<size_t>(o) * (E + 1) + e];
-      all += v;
-      s += o < b ? v : 0;
+  const bool summing = blockIdx.x + 1 == gridDim.x;
+  const int c0 = summing ? B : blockIdx.x * RT_CHUNKS, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int PER = (RT_MAX_BLOCKS + 31) / 32;
+  for (int e = warp; e < E; e += 32) {               // a warp takes an expert: every block's count of it
+    int v[PER];
+    float q[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int b = lane + 32 * i;
+      v[i] = b < B ? hist[static_cast<size_t>(e) * B + b] : 0;
+      q[i] = summing && b < B ? psum[static_cast<size_t>(e) * B + b] : 0.0f;
     }
-    if (b == B) {
-#pragma unroll 8
-      for (int o = lo; o < hi; ++o) q += psum[static_cast<size_t>(o) * E + e];
-      prob[i] = q;
+    int all = 0, s[RT_CHUNKS];
+    float p = 0.0f;
+#pragma unroll
+    for (int c = 0; c < RT_CHUNKS; ++c) s[c] = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      all += v[i];
+      p += q[i];
+#pragma unroll
+      for (int c = 0; c < RT_CHUNKS; ++c) s[c] += lane + 32 * i < c0 + c ? v[i] : 0;
     }
-    before[i] = s;
-    total[i] = all;
+    all = __reduce_add_sync(0xFFFFFFFFu, all);
+    if (summing) {
+      p = group_sum<32>(p);
+      if (lane == 0) prob[e] = p;
+    } else {
+#pragma unroll
+      for (int c = 0; c < RT_CHUNKS; ++c) {
+        s[c] = __reduce_add_sync(0xFFFFFFFFu, s[c]);
+        if (lane == c) base[c * E + e] = s[c];
+      }
+    }
+    if (lane == 0) total[e] = all;
   }
   __syncthreads();
-  int carry = 0;
-  double part_loss = 0.0;
-  for (int e0 = 0; e0 < E; e0 += blockDim.x) {
-    const int e = e0 + threadIdx.x;
-    int s = 0, all = 0;
-    double q = 0.0;
+  const int e = threadIdx.x;                         // E <= 1024
+  const int all = e < E ? total[e] : 0;
+  const int off = block_scan(all, warp_sums);
+  if (summing) {
+    const int rows = warp_sums[32];
     if (e < E) {
-      for (int p = 0; p < parts; ++p) {
-        s += before[p * E + e];
-        all += total[p * E + e];
-        if (b == B) q += prob[p * E + e];
-      }
+      counts[e] = all;
+      offsets[e] = off;
     }
-    const int off = carry + block_scan(all, warp_sums);
-    carry += warp_sums[32];
-    if (e < E) {
-      before[e] = off + s;                           // part 0's place: only this thread reads it
-      if (b == B) {
-        counts[e] = all;
-        offsets[e] = off;
-        part_loss += all * q;
-      }
-    }
-  }
-  if (b == B) {
     int live = 0;
-    for (int o = threadIdx.x; o < B; o += blockDim.x) live += hist[static_cast<size_t>(o) * (E + 1) + E];
+    for (int o = threadIdx.x; o < B; o += blockDim.x) live += hist[static_cast<size_t>(E) * B + o];
     block_scan(live, warp_sums);
     const double n = warp_sums[32];
-    const double all = block_sum(part_loss, sums);
+    const double sum = block_sum(e < E ? static_cast<double>(all) * prob[e] : 0.0, sums);
     if (threadIdx.x == 0) {
       counts[E] = static_cast<int32_t>(n);
-      offsets[E] = carry;
-      if (loss != nullptr) *loss = n > 0.0 ? static_cast<float>(all * E / (static_cast<double>(k) * n * n)) : 0.0f;
+      offsets[E] = rows;
+      if (loss != nullptr) *loss = n > 0.0 ? static_cast<float>(sum * E / (static_cast<double>(k) * n * n)) : 0.0f;
     }
     return;
   }
+  if (e < E)
+#pragma unroll
+    for (int c = 0; c < RT_CHUNKS; ++c) base[c * E + e] += off;
   __syncthreads();
-  const long long first = b * chunk, last = first + chunk < T ? first + chunk : T;
-  route_place(before, ids, pos, row_token, first, last, k);
+  for (int c = 0; c < RT_CHUNKS && c0 + c < B; ++c) {
+    const long long first = (c0 + c) * chunk, last = first + chunk < T ? first + chunk : T;
+    for (long long i = first * k + threadIdx.x; i < last * k; i += blockDim.x) {
+      const int id = ids[i];
+      if (id >= 0) {
+        const int r = pos[i] + base[c * E + id];
+        pos[i] = r;
+        row_token[r] = static_cast<int32_t>(first + static_cast<unsigned>(i - first * k) / static_cast<unsigned>(k));
+      }
+    }
+  }
 }
 
 __device__ __forceinline__ uint32_t pack16(float a, float b, int dtype) {
@@ -663,12 +721,17 @@ combine_backward_kernel(const __half* __restrict__ dout, const __half* __restric
 
 int route_lanes(int E) { return E <= 8 ? 8 : (E <= 16 ? 16 : 32); }
 
-// Blocks of the first kernel: one while a group of lanes has no more than four tokens (the second launch costs more than what
-// more SMs would save), else as many as give every group one.
-int route_blocks(long long T, int E) {
-  const long long groups = RT_THREADS / route_lanes(E);
-  if (T <= 4 * groups) return 1;
-  return static_cast<int>(std::min<long long>(RT_MAX_BLOCKS, (T + groups - 1) / groups));
+// Blocks of the first kernel: one, of 256 threads, while a group of lanes has no more than four tokens (the second launch costs
+// more than what more SMs would save); else as many as give every group of 1024 threads (512: more registers) one.
+int route_threads(int64_t T, int E) {
+  if (T <= 4 * (256 / route_lanes(E))) return 256;
+  return E <= 256 ? 1024 : 512;
+}
+int route_blocks(int64_t T, int E) {
+  const int threads = route_threads(T, E);
+  if (threads == 256) return 1;
+  const int64_t groups = threads / route_lanes(E);
+  return static_cast<int>(std::min<int64_t>(RT_MAX_BLOCKS, std::max<int64_t>(2, (T + groups - 1) / groups)));
 }
 
 size_t elem_bytes(int dtype) { return dtype == SQ_F32 ? 4 : 2; }
@@ -711,17 +774,21 @@ sq_status_t launch_route(const void* logits, int dtype, int64_t T, int E, int64_
   const sq_status_t st = with_shape(E, [&](auto lpt, auto epl) -> sq_status_t {
     constexpr int LPT = decltype(lpt)::value, EPL = decltype(epl)::value;
     const RouteArgs a = {logits, dtype, E, k, T, ld, renorm ? 1 : 0, route_vec(logits, dtype, E, ld, EPL), static_cast<const uint8_t*>(mask)};
-    auto kern = route_kernel<LPT, EPL>;
-    const int smem = (2 * (RT_THREADS / LPT) + 1) * E * 4;
+    constexpr int BIG = EPL <= 8 ? 1024 : 512;
+    const int threads = route_threads(T, E);
+    auto kern = dtype == SQ_F32 ? (threads == 256 ? route_kernel<LPT, EPL, 256, false> : route_kernel<LPT, EPL, BIG, false>)
+                                : (threads == 256 ? route_kernel<LPT, EPL, 256, true> : route_kernel<LPT, EPL, BIG, true>);
+    const int staged = chunk * k <= RT_STAGED;
+    const int smem = ((2 * (threads / LPT) + 1) * E + 2 * threads + (staged ? 2 * RT_STAGED : 0)) * 4;
     if (!ensure_dyn_smem(reinterpret_cast<const void*>(kern), smem)) return SQ_ERR_CUDA;
-    const cudaError_t err = launch_maybe_pdl(kern, dim3(static_cast<unsigned>(B)), dim3(RT_THREADS), static_cast<size_t>(smem), s, a, chunk,
-                                             idsp, static_cast<float*>(gates), posp, hist, psum, cnt, off, rt, static_cast<float*>(loss));
+    const cudaError_t err = launch_maybe_pdl(kern, dim3(static_cast<unsigned>(B)), dim3(static_cast<unsigned>(threads)), static_cast<size_t>(smem), s, a, chunk,
+                                             staged, idsp, static_cast<float*>(gates), posp, hist, psum, cnt, off, rt, static_cast<float*>(loss));
     count_launch();
     return err == cudaSuccess ? SQ_OK : SQ_ERR_CUDA;
   });
   if (st != SQ_OK || B == 1) return st;
-  const int smem = 3 * std::max(1, 1024 / E) * E * 4;
-  const cudaError_t err = launch_dependent(route_finish_kernel, dim3(static_cast<unsigned>(B + 1)), dim3(1024), static_cast<size_t>(smem), s, B,
+  const int smem = (RT_CHUNKS + 2) * E * 4;
+  const cudaError_t err = launch_dependent(route_finish_kernel, dim3(static_cast<unsigned>((B + RT_CHUNKS - 1) / RT_CHUNKS + 1)), dim3(1024), static_cast<size_t>(smem), s, B,
                                            E, k, static_cast<long long>(T), chunk, static_cast<const int32_t*>(hist),
                                            static_cast<const float*>(psum), static_cast<const int32_t*>(idsp), posp, cnt, off, rt,
                                            static_cast<float*>(loss));
