@@ -28,7 +28,7 @@ namespace {
 
 constexpr int RT_MAX_BLOCKS = 148;                   // the second kernel reads every block's counts, five to a lane
 constexpr int RT_STAGED = 4096;                      // slots of a block whose expert and rank stay in shared memory
-constexpr int RT_CHUNKS = 4;                         // blocks of the first kernel that one of the second finishes
+constexpr int RT_CHUNKS = 1;                         // blocks of the first kernel that one of the second finishes
 constexpr uint32_t RT_KEY_NINF = 0x007FFFFFu;        // route_key(-inf): not above it is not usable
 constexpr float RT_NINF = -__builtin_huge_valf();
 
@@ -110,6 +110,13 @@ __device__ __forceinline__ float route_exp(float x, float m) { return x == m ? 1
 // Logits of 16 bits and their place in one key: larger logits first, then lower places, and no two alike.
 __device__ __forceinline__ uint32_t route_key16(float x, int e) { return (route_key(x) & 0xFFFFE000u) | static_cast<uint32_t>(0x1FFF - e); }
 
+constexpr float RT_LOG2E = 1.44269504088896340736f;
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 template <int LPT>
 __device__ __forceinline__ float group_max(float v) {
 #pragma unroll
@@ -132,10 +139,19 @@ __device__ __forceinline__ bool route_softmax(const float (&x)[EPL], float (&p)[
   m = group_max<LPT>(m);
   const bool usable = m > RT_NINF;
   float s = 0.0f;
+  if (__all_sync(0xFFFFFFFFu, m < -RT_NINF)) {
+    const float from = usable ? m : 0.0f;            // (all -inf: zeros)
 #pragma unroll
-  for (int i = 0; i < EPL; ++i) {
-    p[i] = usable && x[i] > RT_NINF ? route_exp(x[i], m) : 0.0f;
-    s += p[i];
+    for (int i = 0; i < EPL; ++i) {
+      p[i] = exp2_fast((x[i] - from) * RT_LOG2E);
+      s += p[i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      p[i] = usable && x[i] > RT_NINF ? route_exp(x[i], m) : 0.0f;
+      s += p[i];
+    }
   }
   s = group_sum<LPT>(s);
   inv = usable ? 1.0f / s : 0.0f;
@@ -166,6 +182,25 @@ __device__ __forceinline__ void route_select(const float (&x)[EPL], int sub, int
   for (int i = 0; i < EPL; ++i) key[i] = KEY16 ? route_key16(x[i], sub * EPL + i) : route_key(x[i]);
   uint32_t mine = 0;
   int where = 0;
+  if (KEY16 && EPL >= 4 && EPL <= 8) {
+    // A lane's keys in order, largest first (odd-even transposition); the largest of the heads goes, and its lane's keys move up.
+#pragma unroll
+    for (int r = 0; r < EPL; ++r)
+#pragma unroll
+      for (int i = r & 1; i + 1 < EPL; i += 2) {
+        const uint32_t hi = max(key[i], key[i + 1]), lo = min(key[i], key[i + 1]);
+        key[i] = hi;
+        key[i + 1] = lo;
+      }
+    for (int j = 0; j < k; ++j) {
+      const uint32_t top = __reduce_max_sync(0xFFFFFFFFu, key[0]);
+      const bool pop = key[0] == top;
+#pragma unroll
+      for (int i = 0; i + 1 < EPL; ++i) key[i] = pop ? key[i + 1] : key[i];
+      key[EPL - 1] = pop ? 0u : key[EPL - 1];
+      if (sub == j) mine = top;
+    }
+  } else
   for (int j = 0; j < k; ++j) {
     uint32_t best = key[0];
 #pragma unroll
@@ -477,6 +512,12 @@ route_backward_kernel(const RouteArgs a, const int32_t* __restrict__ ids, const 
                       const int32_t* __restrict__ counts, const float* __restrict__ dgates, const float* __restrict__ dloss,
                       void* dlogits, long long ld_d, int vec_d) {
   griddep_launch_dependents();
+  // A group's row of what its slots add to the logits' gradients: all zeros between tokens.
+  __shared__ __align__(16) float rows[256 / LPT][LPT * EPL];
+  float* add_row = rows[threadIdx.x / LPT];
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) add_row[(threadIdx.x % LPT) * EPL + i] = 0.0f;
+  __syncwarp();
   griddep_wait();
   const int sub = threadIdx.x % LPT, E = a.E, k = a.k;
   const long long groups = static_cast<long long>(gridDim.x) * (blockDim.x / LPT);
@@ -515,15 +556,13 @@ route_backward_kernel(const RouteArgs a, const int32_t* __restrict__ ids, const 
     float add = dg;
     if (a.renorm) add = g * (dg - group_sum<LPT>(g * dg));
     float extra[EPL];
+    const bool put = id >= 0 && id < E;              // the token's experts differ: no two lanes write one place
+    if (put) add_row[id] = add;
+    __syncwarp();
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) extra[i] = 0.0f;
-    for (int j = 0; j < k; ++j) {
-      const int e = __shfl_sync(0xFFFFFFFFu, id, j, LPT) - sub * EPL;
-      const float v = __shfl_sync(0xFFFFFFFFu, add, j, LPT);
-#pragma unroll
-      for (int i = 0; i < EPL; ++i)
-        if (e == i) extra[i] += v;
-    }
+    for (int i = 0; i < EPL; ++i) extra[i] = add_row[sub * EPL + i];
+    __syncwarp();
+    if (put) add_row[id] = 0.0f;
     if (!a.renorm) {
 #pragma unroll
       for (int i = 0; i < EPL; ++i) { d[i] += extra[i]; extra[i] = 0.0f; }
