@@ -145,6 +145,8 @@ __device__ __forceinline__ uint32_t high_nibbles(uint32_t w, const NibbleConsts&
   return x;
 }
 
+__device__ const uint4 g_zero_words[4] = {};
+
 template <int RB, int NT, int GROUP, bool BIAS, bool EXPERTS>
 __global__ void __launch_bounds__(GS_THREADS, 2)
 gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ GsArgs a, int R, int splits) {
@@ -196,7 +198,6 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
   // Cursor of the copies: the steps left of its tile, and the tile's weights and scales (of this lane's pair of channels).
   int ileft = 0, itiles = cw > 0 ? my_tiles : 0, itile = cid, islot = 0, ix = 0, iy = 0;
   const __half *is = nullptr, *ib = nullptr;
-  bool iin = false;
   const size_t step_s = static_cast<size_t>(GS_WARPS * CHUNKS) * N;
   const uint32_t put_s = smem_u32(ring) + L::OFF_S + lane * 4;
   auto issue = [&]() {
@@ -205,8 +206,7 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
       const int e = EXPERTS ? chunk_expert(first, a.E, chunk) : 0;
       const int row0 = (itile - chunk * ctiles) * R;
       iy = e * N + row0;
-      iin = 2 * lane < min(R, N - row0);
-      const size_t so = (static_cast<size_t>(e) * G + ks0 * CHUNKS) * N + row0 + 2 * lane;
+      const size_t so = (static_cast<size_t>(e) * G + ks0 * CHUNKS) * N + row0 + min(2 * lane, min(R, N - row0) - 2);
       is = a.sg + so;
       if (BIAS) ib = a.bg + so;
       ix = ks0 * 64;
@@ -220,22 +220,15 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
         mbar_arrive_expect_tx(&full[islot], static_cast<uint32_t>(R * 64));
         tma_load_2d(ring + islot * L::W_SLOT, &tmap_w, &full[islot], ix, iy);
       }
-      if (iin) {
+      if (RB == 4 || lane < 8 * RB) {
         const uint32_t d = put_s + islot * (2 * L::S_SLOT);
-        if (!(ragged && ileft == 0)) {
 #pragma unroll
-          for (int c = 0; c < CHUNKS; ++c) {
-            cp_async_4(d + c * (2 * L::ROWS), is + static_cast<size_t>(c) * N);
-            if (BIAS) cp_async_4(d + c * (2 * L::ROWS) + L::S_SLOT, ib + static_cast<size_t>(c) * N);
-          }
-        } else {
+        for (int c = 0; c < CHUNKS; ++c) {
           // A group behind the last one takes the last one's: its tokens are zeros, its scales have to be finite.
-#pragma unroll
-          for (int c = 0; c < CHUNKS; ++c) {
-            const size_t o = static_cast<size_t>(min(c, G - 1 - (nks - 1) * CHUNKS)) * N;
-            cp_async_4(d + c * (2 * L::ROWS), is + o);
-            if (BIAS) cp_async_4(d + c * (2 * L::ROWS) + L::S_SLOT, ib + o);
-          }
+          size_t o = static_cast<size_t>(c) * N;
+          if (CHUNKS > 1 && c > 0 && ragged && ileft == 0) o = static_cast<size_t>(min(c, G - 1 - (nks - 1) * CHUNKS)) * N;
+          cp_async_4(d + c * (2 * L::ROWS), is + o);
+          if (BIAS) cp_async_4(d + c * (2 * L::ROWS) + L::S_SLOT, ib + o);
         }
       }
       is += step_s;
@@ -279,16 +272,14 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
       xtile += ncl;
       --xtiles;
     }
-    if (!(ragged && xleft == 1)) {
+    // Channels behind the last are read as zeros.
+    const bool last = ragged && xleft == 1;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)                    // word i % WPL of chunk i / WPL
-        xn[i] = __ldg(reinterpret_cast<const uint4*>(xat[n] + (i / WPL) * GROUP + 8 * (i % WPL)));
-    } else {
+    for (int c = 0; c < CHUNKS; ++c) {
+      const uint4* p = reinterpret_cast<const uint4*>(xat[n] + c * GROUP);
+      if (last && (nks - 1) * 128 + c * GROUP + 8 * WPL * t >= K) p = g_zero_words;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int k = (i / WPL) * GROUP + 8 * (i % WPL);
-        xn[i] = (nks - 1) * 128 + k + 8 * WPL * t < K ? __ldg(reinterpret_cast<const uint4*>(xat[n] + k)) : make_uint4(0u, 0u, 0u, 0u);
-      }
+      for (int j = 0; j < WPL; ++j) xn[c * WPL + j] = __ldg(p + j);
     }
     xat[n] += GS_WARPS * 128;
     if (n == NT - 1) --xleft;
@@ -395,7 +386,6 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
         phase ^= 1;
       }
       __syncwarp();                                  // every lane has read the slot
-      ok = __all_sync(0xFFFFFFFFu, ok);
       if (ok) issue();
     }
     // The warps' sums over K, added up in a fixed order.

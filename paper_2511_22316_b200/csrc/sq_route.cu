@@ -619,10 +619,10 @@ combine_kernel(const __half* __restrict__ Y, long long M, const int32_t* __restr
   griddep_launch_dependents();
   griddep_wait();
   constexpr int W = VEC ? 8 : 1;
-  const long long nc = N / W, total = T * nc;
-  for (long long i = blockIdx.x * static_cast<long long>(blockDim.x) + threadIdx.x; i < total;
-       i += static_cast<long long>(gridDim.x) * blockDim.x) {
-    const long long t = i / nc, c = (i - t * nc) * W;
+  // A block takes 256 W channels of one token: nothing to divide, and every load goes out at once.
+  const long long c = (blockIdx.x * 256ll + threadIdx.x) * W;
+  if (c >= N) return;
+  for (long long t = blockIdx.y; t < T; t += gridDim.y) {
     float acc[W];
 #pragma unroll
     for (int w = 0; w < W; ++w) acc[w] = 0.0f;
@@ -856,12 +856,9 @@ sq_status_t launch_route_backward(const void* logits, int dtype, int64_t T, int 
 
 sq_status_t launch_combine(const void* Y, int64_t M, const void* pos, const void* gates, int64_t T, int k, int64_t N, void* out,
                            cudaStream_t s) {
-  const int sms = sm_count();
-  if (sms <= 0) return SQ_ERR_CUDA;
   const bool vec = N % 8 == 0;
-  const long long work = T * (vec ? N / 8 : N);
-  const unsigned grid = static_cast<unsigned>(std::min<long long>((work + 255) / 256, static_cast<long long>(sms) * 8));
-  const cudaError_t err = launch_maybe_pdl(vec ? combine_kernel<true> : combine_kernel<false>, dim3(grid), dim3(256), 0, s,
+  const dim3 grid(static_cast<unsigned>(((vec ? N / 8 : N) + 255) / 256), static_cast<unsigned>(std::min<int64_t>(T, 65535)));
+  const cudaError_t err = launch_maybe_pdl(vec ? combine_kernel<true> : combine_kernel<false>, grid, dim3(256), 0, s,
                                            static_cast<const __half*>(Y), static_cast<long long>(M), static_cast<const int32_t*>(pos),
                                            static_cast<const float*>(gates), static_cast<long long>(T), k, static_cast<long long>(N),
                                            static_cast<__half*>(out));
