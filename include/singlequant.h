@@ -288,8 +288,10 @@ sq_status_t sq_linear_grouped(const sq_rotation_t* const* rots, int32_t E, const
  *   sg     fp16 [G x N], group-major: the scales of all channels of one group lie side by side
  *   bg     fp16 [G x N] or NULL (no offset).  A checkpoint with unsigned codes u and zero points z,
  *          w = s (u - z), has code = u - 8 (u ^ 8 as a nibble) and bg = s (8 - z).
- * sg and bg are finite and |code * sg + bg| < 65504: the kernels that multiply on the tensor cores round
- * each weight once to fp16 (one fused multiply-add), the others keep it in fp32.  Sums are fp32.
+ * sg and bg are finite and |code * sg + bg| < 65504: the kernels for more than 8 rows (16 of a small layer)
+ * round each weight once to fp16 (one fused multiply-add), the others do not round it.  Sums are fp32.
+ * A token with an infinity or a NaN gets infinities or NaN in its own row (which of them may differ from
+ * kernel to kernel); the other rows do not depend on it.
  * ------------------------------------------------------------------------------------------- */
 
 /* Offline: rotate the rows of W (fp32), quantise each group, store in the weight-only order.
@@ -308,7 +310,7 @@ sq_status_t sq_pack_weight_gs(const sq_rotation_t* rot_or_null, const void* W, i
 
 /* Y[t,c] = fp16(sum_k Z16[t,k] * w[c,k]).
  *   Z16 DEVICE fp16 [M x K]     Wq, sg, bg as above     Y DEVICE fp16 [M x N] (out)
- * K % 8 == 0, K <= 65536.  The fast kernels take K % 32 == 0 with N even up to 16 tokens, and K % 64 == 0 above;
+ * K % 8 == 0, K <= 65536.  The fast kernels take K % 32 == 0 (the one for the fewest tokens N even besides);
  * other shapes run a plain fp32 kernel.  The order of the sums is fixed for given M, N and K.  Ordering in the
  * stream as sq_w4a4_gemm: Wq, sg and bg may be requested while the kernel before still runs. */
 sq_status_t sq_w4a16_gemm_gs(const void* Z16, const void* Wq, const void* sg, const void* bg_or_null, int64_t M,

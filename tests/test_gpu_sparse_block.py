@@ -86,6 +86,22 @@ def test_route(T, E, k, renorm, dtype):
     Routed(x, dtype, k, renorm, mask, ld=E if T % 3 else E + 5).check()
 
 
+def test_route_of_more_slots_than_stay_on_chip():
+    """More than 4096 slots of a block: experts and ranks go through the outputs instead."""
+    rng = np.random.default_rng(0)
+    Routed(rng.standard_normal((90000, 8)) + rng.standard_normal(8), "fp32", 8, False, rng.random(90000) < 0.9).check()
+
+
+def test_combine_without_rows():
+    import torch
+    pos, gates, out = dev(np.zeros((3, 2), np.int32)), dev(np.ones((3, 2), np.float32)), Guarded(3 * 16 * 2)
+    sq.sq_combine(None, 0, pos, gates, 3, 2, 16, out)
+    dg = Guarded(3 * 2 * 4)
+    sq.sq_combine_backward(dev(np.ones((3, 16), np.float16)), None, 0, pos, gates, 3, 2, 16, None, dg)
+    torch.cuda.synchronize()
+    assert not out.numpy(np.uint16, (3, 16)).any() and not dg.numpy(np.uint32, (3, 2)).any()
+
+
 @pytest.mark.parametrize("E,k", [(8, 3), (16, 4), (40, 8), (300, 5)])
 @pytest.mark.parametrize("T", [3, 400])
 def test_equal_logits_go_to_the_lowest_index(T, E, k):
