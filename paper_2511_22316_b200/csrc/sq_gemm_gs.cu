@@ -168,7 +168,6 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
   const int cw = ks1 > ks0 ? (ks1 - ks0 + GS_WARPS - 1) / GS_WARPS : 0;      // this warp's steps of a tile
   // The step whose channels end before 128 of them, if it is this warp's: always the last of its steps.
   const bool ragged = (K & 127) != 0 && cw > 0 && ks0 + (cw - 1) * GS_WARPS == nks - 1;
-  const int ctiles = (N + R - 1) / R;
   unsigned char* ring = smem + warp * L::RING;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::OFF_BAR) + warp * L::DEPTH;
   if (lane == 0) {
@@ -177,13 +176,22 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
     mbar_fence_init();
   }
   __syncwarp();
-  int tiles = ctiles;
+  // Tiles of blocks of 16 channels.  Dense: a run of them for every thread block, as even as can be, cut into tiles of up to RB (1 x
+  // 8192 -> 28672 29.2 -> 26.9 us against whole tiles dealt out in turn).  Experts: the tiles of R channels of all chunks of rows in
+  // one list, dealt out in turn.
+  const int nb = (N + 15) / 16, ctiles = (N + R - 1) / R;
+  int my_tiles = 0, run0 = 0, run1 = 0;              // experts: how many tiles; dense: a run of blocks
   if constexpr (EXPERTS) {
     griddep_wait();                                  // the offsets come from the router
     expert_chunks(a, 8 * NT, first);
-    tiles = first[a.E] * ctiles;
+    const int tiles = first[a.E] * ctiles;           // (the launcher has seen to it that they fit 32 bits)
+    my_tiles = cid < tiles ? (tiles - cid + ncl - 1) / ncl : 0;
+  } else {
+    run0 = static_cast<int>(static_cast<long long>(nb) * cid / ncl);
+    run1 = static_cast<int>(static_cast<long long>(nb) * (cid + 1) / ncl);
+    my_tiles = (run1 - run0 + RB - 1) / RB;
   }
-  const int my_tiles = cid < tiles ? (tiles - cid + ncl - 1) / ncl : 0;
+  auto dense_size = [&](int from, int left) { return (run1 - from + left - 1) / left; };      // of the first of `left` tiles
   const uint32_t limit = wait_limit();
 
   // Where this lane reads its words of row g of a block, by group: 16-byte piece p of row r lies at p ^ (r >> 1 & 3).
@@ -196,7 +204,7 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
   const uint32_t take_s = smem_u32(ring) + L::OFF_S + g * 2;
 
   // Cursor of the copies: the steps left of its tile, and the tile's weights and scales (of this lane's pair of channels).
-  int ileft = 0, itiles = cw > 0 ? my_tiles : 0, itile = cid, islot = 0, ix = 0, iy = 0;
+  int ileft = 0, itiles = cw > 0 ? my_tiles : 0, itile = EXPERTS ? cid : run0, isize = 0, islot = 0, ix = 0, iy = 0;
   const __half *is = nullptr, *ib = nullptr;
   const size_t step_s = static_cast<size_t>(GS_WARPS * CHUNKS) * N;
   const uint32_t put_s = smem_u32(ring) + L::OFF_S + lane * 4;
@@ -204,21 +212,28 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
     if (ileft == 0 && itiles > 0) {
       const int chunk = EXPERTS ? itile / ctiles : 0;
       const int e = EXPERTS ? chunk_expert(first, a.E, chunk) : 0;
-      const int row0 = (itile - chunk * ctiles) * R;
-      iy = e * N + row0;
-      const size_t so = (static_cast<size_t>(e) * G + ks0 * CHUNKS) * N + row0 + min(2 * lane, min(R, N - row0) - 2);
+      if (!EXPERTS) isize = dense_size(itile, itiles);
+      const int row0 = EXPERTS ? (itile - chunk * ctiles) * R : 16 * itile;
+      iy = e * N + row0 + (EXPERTS ? 0 : 16 * lane);           // dense: lane b < isize loads block b
+      const size_t so = (static_cast<size_t>(e) * G + ks0 * CHUNKS) * N + row0 + min(2 * lane, min(EXPERTS ? R : 16 * isize, N - row0) - 2);
       is = a.sg + so;
       if (BIAS) ib = a.bg + so;
       ix = ks0 * 64;
       ileft = cw;
-      itile += ncl;
+      itile += EXPERTS ? ncl : isize;
       --itiles;
     }
     if (ileft > 0) {
       --ileft;
-      if (lane == 0) {
-        mbar_arrive_expect_tx(&full[islot], static_cast<uint32_t>(R * 64));
-        tma_load_2d(ring + islot * L::W_SLOT, &tmap_w, &full[islot], ix, iy);
+      if constexpr (EXPERTS) {                       // one box of a whole tile's rows
+        if (lane == 0) {
+          mbar_arrive_expect_tx(&full[islot], L::W_SLOT);
+          tma_load_2d(ring + islot * L::W_SLOT, &tmap_w, &full[islot], ix, iy);
+        }
+      } else {
+        if (lane == 0) mbar_arrive_expect_tx(&full[islot], static_cast<uint32_t>(isize * 1024));
+        __syncwarp();
+        if (lane < isize) tma_load_2d(ring + islot * L::W_SLOT + lane * 1024, &tmap_w, &full[islot], ix, iy);
       }
       if (RB == 4 || lane < 8 * RB) {
         const uint32_t d = put_s + islot * (2 * L::S_SLOT);
@@ -245,12 +260,14 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
   // Cursor of the tokens, eight rows ahead of the products.  Columns of an MMA that are no row of the tile repeat another row (its
   // sums are not stored).
   int xleft = 0, xtiles = cw > 0 ? my_tiles : 0, xtile = cid;
+  bool xaimed = false;
   const __half *xrow[NT], *xat[NT];
   uint4 xn[4];
   auto fetch = [&](int n) {
     if (n == 0 && xleft == 0) {
       if (xtiles == 0) return;
-      if (EXPERTS || xtile == cid) {
+      if (EXPERTS || !xaimed) {
+        xaimed = true;
         long long lo = 0, hi = a.M;
         if constexpr (EXPERTS) {
           const int chunk = xtile / ctiles, e = chunk_expert(first, a.E, chunk);
@@ -291,9 +308,11 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
   int slot = 0;
   uint32_t phase = 0;
   bool ok = true;
-  for (int tl = 0, tile = cid; tl < my_tiles; ++tl, tile += ncl) {
+  for (int tl = 0, tile = EXPERTS ? cid : run0; tl < my_tiles; ++tl) {
     const int chunk = EXPERTS ? tile / ctiles : 0;
-    const int row0 = (tile - chunk * ctiles) * R, rows = min(R, N - row0);
+    const int size = EXPERTS ? RB : dense_size(tile, my_tiles - tl);
+    const int row0 = EXPERTS ? (tile - chunk * ctiles) * R : 16 * tile, rows = min(EXPERTS ? R : 16 * size, N - row0);
+    tile += EXPERTS ? ncl : size;
     float acc[RB][NT][4];                            // in units of 2^-24
 #pragma unroll
     for (int b = 0; b < RB; ++b)
@@ -331,11 +350,12 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
           ok = mbar_wait(&full[slot], phase, GS_FULL, ok ? limit : 65536u) && ok;
           __syncwarp();                              // the other lanes' scales
         }
-        // Two blocks of 16 channels side by side: four chains of MMAs (a chain takes 21 cycles a link and up, the tensor pipe 8).
-        constexpr int PB = RB > 1 ? 2 : 1;
+        // Experts: two blocks of channels side by side, as all tiles have four (a dense tile may have three: 26.9 us, and 30.2 in twos,
+        // for 1 x 8192 -> 28672).
+        constexpr int PB = EXPERTS ? 2 : 1;
 #pragma unroll
         for (int b0 = 0; b0 < RB; b0 += PB) {
-          if (RB > PB && 16 * b0 >= rows) break;
+          if (EXPERTS ? 16 * b0 >= rows : RB > PB && b0 >= size) break;
           const uint32_t d = slot * L::W_SLOT + b0 * 1024, ds = take_s + slot * 2 * L::S_SLOT + b0 * 32;
 #pragma unroll
           for (int c = 0; c < CHUNKS; ++c) {
@@ -541,7 +561,7 @@ sq_status_t launch_quant_groups(const void* X, bool f32, int64_t rows, int64_t r
 namespace {
 
 template <int RB, int NT, int GROUP, bool BIAS, bool EXPERTS>
-sq_status_t launch_stream_as(const GsArgs& a, int R, int splits, int grid, cudaStream_t s) {
+sq_status_t launch_stream_as(const GsArgs& a, int splits, int grid, cudaStream_t s) {
   using L = GsStream<RB, NT, GROUP>;
   auto kern = gs_stream_kernel<RB, NT, GROUP, BIAS, EXPERTS>;
   if (!ensure_dyn_smem(reinterpret_cast<const void*>(kern), L::BYTES)) return SQ_ERR_CUDA;
@@ -550,78 +570,69 @@ sq_status_t launch_stream_as(const GsArgs& a, int R, int splits, int grid, cudaS
   CUtensorMap mw;
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(a.K / 2), static_cast<cuuint64_t>(a.N * std::max(a.E, 1))};
   const cuuint64_t strides[1] = {static_cast<cuuint64_t>(a.K / 2)};
-  const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(R)};
+  const cuuint32_t box[2] = {64, EXPERTS ? L::ROWS : 16};
   const cuuint32_t estr[2] = {1, 1};
   if (enc(&mw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(a.Wq), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
           CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return SQ_ERR_CUDA;
   const cudaError_t err = launch_cluster_maybe_pdl(kern, dim3(static_cast<unsigned>(grid)), dim3(GS_THREADS), static_cast<size_t>(L::BYTES),
-                                                   s, static_cast<unsigned>(splits), mw, a, R, splits);
+                                                   s, static_cast<unsigned>(splits), mw, a, 16 * RB, splits);
   count_launch();
   return err == cudaSuccess ? SQ_OK : SQ_ERR_CUDA;
 }
-// Experts take eight rows at a time and the largest tiles: there are enough of them.
+// `rb`: blocks of 16 channels that a tile has to hold (experts take eight rows at a time and the largest tiles).
 template <int GROUP, bool BIAS, bool EXPERTS>
-sq_status_t launch_stream_rows(const GsArgs& a, int nt, int R, int splits, int grid, cudaStream_t s) {
+sq_status_t launch_stream_rows(const GsArgs& a, int nt, int rb, int splits, int grid, cudaStream_t s) {
   if constexpr (!EXPERTS) {
-    if (R <= 16 && nt == 1) return launch_stream_as<1, 1, GROUP, BIAS, EXPERTS>(a, R, splits, grid, s);
-    if (R <= 32 && nt == 1) return launch_stream_as<2, 1, GROUP, BIAS, EXPERTS>(a, R, splits, grid, s);
-    if (R <= 16) return launch_stream_as<1, 2, GROUP, BIAS, EXPERTS>(a, R, splits, grid, s);
-    if (nt == 2) return launch_stream_as<2, 2, GROUP, BIAS, EXPERTS>(a, R, splits, grid, s);
+    if (rb == 1 && nt == 1) return launch_stream_as<1, 1, GROUP, BIAS, EXPERTS>(a, splits, grid, s);
+    if (rb == 2 && nt == 1) return launch_stream_as<2, 1, GROUP, BIAS, EXPERTS>(a, splits, grid, s);
+    if (rb == 1) return launch_stream_as<1, 2, GROUP, BIAS, EXPERTS>(a, splits, grid, s);
+    if (nt == 2) return launch_stream_as<2, 2, GROUP, BIAS, EXPERTS>(a, splits, grid, s);
   }
-  return launch_stream_as<4, 1, GROUP, BIAS, EXPERTS>(a, R, splits, grid, s);
+  return launch_stream_as<4, 1, GROUP, BIAS, EXPERTS>(a, splits, grid, s);
 }
 template <bool EXPERTS>
-sq_status_t launch_stream_any(const GsArgs& a, int nt, int R, int splits, int grid, cudaStream_t s) {
+sq_status_t launch_stream_any(const GsArgs& a, int nt, int rb, int splits, int grid, cudaStream_t s) {
   if (a.group == 128)
-    return a.bg ? launch_stream_rows<128, true, EXPERTS>(a, nt, R, splits, grid, s) : launch_stream_rows<128, false, EXPERTS>(a, nt, R, splits, grid, s);
+    return a.bg ? launch_stream_rows<128, true, EXPERTS>(a, nt, rb, splits, grid, s) : launch_stream_rows<128, false, EXPERTS>(a, nt, rb, splits, grid, s);
   if (a.group == 64)
-    return a.bg ? launch_stream_rows<64, true, EXPERTS>(a, nt, R, splits, grid, s) : launch_stream_rows<64, false, EXPERTS>(a, nt, R, splits, grid, s);
-  return a.bg ? launch_stream_rows<32, true, EXPERTS>(a, nt, R, splits, grid, s) : launch_stream_rows<32, false, EXPERTS>(a, nt, R, splits, grid, s);
+    return a.bg ? launch_stream_rows<64, true, EXPERTS>(a, nt, rb, splits, grid, s) : launch_stream_rows<64, false, EXPERTS>(a, nt, rb, splits, grid, s);
+  return a.bg ? launch_stream_rows<32, true, EXPERTS>(a, nt, rb, splits, grid, s) : launch_stream_rows<32, false, EXPERTS>(a, nt, rb, splits, grid, s);
 }
-
-int even_rows(int64_t N, int64_t tiles) { return static_cast<int>(std::max<int64_t>(2, (N + 2 * tiles - 1) / (2 * tiles) * 2)); }
 
 sq_status_t launch_stream(const GsArgs& a, cudaStream_t s) {
   const int sms = sm_count();
   if (sms <= 0) return SQ_ERR_CUDA;
   const int slots = 2 * sms, nks = (a.K + 127) / 128;
-  if (a.E > 0) {
-    // Eight rows of an expert and up to 64 channels make a tile, and the tiles are dealt out to all blocks (sixteen tokens on eight
-    // experts, 4096 -> 14336, with 16 / 32 / 64 channels: 120 / 80 / 58 us).
-    const int64_t chunks = std::min<int64_t>(a.E, a.M);
-    const int R = std::min(64, std::max(16, even_rows(a.N, std::max<int64_t>(1, slots / chunks))));
-    return launch_stream_any<true>(a, 1, R, 1, slots, s);
-  }
-  const int nt = a.M <= 8 ? 1 : 2, cap = nt == 1 ? 64 : 32;
-  // Time of a call in us, fitted to R of 14 to 64 with K in 1 to 8 parts on 1 to 8 rows of five shapes, 4096 x 4096 to 8192 x 28672
-  // (10 % off): a step of 128 channels costs something by itself, something for its rows and something for its (pairs of) blocks of 16
-  // channels, more with small groups, and a third less where an SM has one block.  K over a cluster costs 1.5 us and has to fit the
-  // chip at once: 5 x 14336 -> 4096 with K in 1 / 2 / 4 parts 16.2 / 12.5 / 12.4 us, but 17.7 with 74 clusters of four.
+  // Experts: eight rows and 64 channels make a tile (sixteen tokens on eight experts, 4096 -> 14336, with 16 / 32 / 64 channels: 120 /
+  // 80 / 58 us).
+  if (a.E > 0) return launch_stream_any<true>(a, 1, 4, 1, slots, s);
+  const int nt = a.M <= 8 ? 1 : 2, cap = nt == 1 ? 4 : 2;
+  const int64_t nb = (a.N + 15) / 16;
+  // Time of a call in us, fitted to one to eight rows of five shapes, 4096 x 4096 to 8192 x 28672, with K in 1 to 8 parts (10 % off): a
+  // step of 128 channels costs something by itself, something for its rows and something for its blocks of 16 channels, more with
+  // small groups, and a third less where an SM has one block.  K over a cluster costs 1.5 us and has to fit the chip at once: 5 x
+  // 14336 -> 4096 with K in 1 / 2 / 4 parts 16.2 / 12.5 / 12.4 us, but 17.7 with 74 clusters of four.
   const double unit = a.group == 128 ? 0.36 : (a.group == 64 ? 0.45 : 0.54);
-  int best_r = 0, best_s = 1, best_grid = 0;
+  int best_rb = 0, best_s = 1, best_grid = 0;
   double best = 0.0;
   for (int sp = 1; sp <= 8 && nks / sp >= (sp == 1 ? 1 : 8); sp *= 2) {
     const int room = sp == 1 ? slots : (sp == 2 ? slots - slots / 16 : slots - slots / 8);       // blocks that clusters find place for
-    for (int waves = 1; waves <= (sp == 1 ? 8 : 1); ++waves) {
-      for (int half = 0; half < 2; ++half) {         // one block per SM, or two
-        const int want = even_rows(a.N, static_cast<int64_t>((half ? room / 2 : room) / sp) * waves);
-        if (want > cap && (half || sp > 1 || waves < 8)) continue;
-        const int r = std::min(want, cap);
-        const int64_t tiles = (a.N + r - 1) / r, rounds = (tiles * sp + slots - 1) / slots;
-        const int blocks = r <= 16 ? 1 : (r + 31) / 32 * 2;
-        const double cost = static_cast<double>(rounds) * (((nks + sp - 1) / sp + GS_WARPS - 1) / GS_WARPS) * (unit * blocks * nt + 0.31 + 0.024 * a.M) *
-                                (tiles * sp <= sms ? 0.67 : 1.0) + (sp > 1 ? 1.5 : 0.0);
-        if (best_r == 0 || cost < best) {
-          best = cost;
-          best_r = r;
-          best_s = sp;
-          best_grid = static_cast<int>(std::min<int64_t>(tiles * sp, slots));
-        }
+    for (int half = 0; half < 2; ++half) {           // two blocks per SM, or one
+      const int64_t ncl = std::min<int64_t>(nb, (half ? room / 2 : room) / sp), per = (nb + ncl - 1) / ncl;
+      if (sp > 1 && per > cap) continue;             // one tile for a cluster
+      const int64_t cuts = (per + cap - 1) / cap;
+      const double cost = (((nks + sp - 1) / sp + GS_WARPS - 1) / GS_WARPS) * (unit * nt * per + cuts * (0.31 + 0.024 * a.M)) *
+                              (ncl * sp <= sms ? 0.67 : 1.0) + (sp > 1 ? 1.5 : 0.0);
+      if (best_rb == 0 || cost < best) {
+        best = cost;
+        best_rb = per == 1 ? 1 : (per == 2 || nt == 2 ? 2 : 4);
+        best_s = sp;
+        best_grid = static_cast<int>(ncl * sp);
       }
     }
   }
-  return launch_stream_any<false>(a, nt, best_r, best_s, best_grid, s);
+  return launch_stream_any<false>(a, nt, best_rb, best_s, best_grid, s);
 }
 
 // Rows of a token tile of the CTA-pair kernel for experts (a multiple of 32 up to 256), as for a dense product: waves of tiles,
@@ -649,7 +660,9 @@ sq_status_t launch_gemm_gs(const GsArgs& a, void* workspace, cudaStream_t s) {
   // -> 4096 7.5 us and 9.3, but 16 x 4096 -> 14336 19.4 and 14.9.
   const bool few = a.E > 0 ? a.M <= 8 * static_cast<int64_t>(a.E) : a.M <= 8 || (a.M <= 16 && a.N * a.K <= 30000000);
   const int64_t kMax = (1ll << 31) - 1024;           // 32-bit coordinates of a tile in the weights and in the rows
-  if (a.K % 32 == 0 && a.N % 2 == 0 && few && a.N * std::max(a.E, 1) <= kMax) return launch_stream(a, s);
+  if (a.K % 32 == 0 && a.N % 2 == 0 && few && a.N * std::max(a.E, 1) <= kMax &&
+      (a.N / 16 + 1) * (a.E + a.M / 8 + 1) <= kMax)
+    return launch_stream(a, s);
   if (a.K % 32 == 0 && a.M <= kMax && a.N * std::max(a.E, 1) <= kMax) {
     if (a.E == 0) return launch_wo_gemm_groups(a, 0, s);
     GsArgs b = a;
