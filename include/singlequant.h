@@ -368,7 +368,8 @@ enum { SQ_F16 = 0, SQ_BF16 = 1, SQ_F32 = 2 };
  *   row_token     DEVICE int32 [T k] (out): the token of each row; entries from offsets[E] on are left as they were
  *   pos           DEVICE int32 [T x k] (out): the row of each token's slot
  *   loss_or_null  DEVICE fp32 [1] (out)
- *   workspace     DEVICE, sq_route_workspace_bytes(T, E) bytes (at most 2 MB), 256-byte aligned
+ *   workspace     DEVICE, sq_route_workspace_bytes(T, E) bytes (at most 2 MB), 256-byte aligned; nothing in it needs
+ *                 clearing, but calls that overlap on the GPU need one each
  * An expert whose logit is -inf or NaN has p = 0 and is never selected; slots that are left over, and all slots of
  * padding and of tokens without any usable logit (which do not count in n either), get id -1, gate 0, pos -1.
  * Logits of +inf share p = 1.  T k < 2^31.  T = 0 writes counts, offsets and loss.  The results do not depend on the

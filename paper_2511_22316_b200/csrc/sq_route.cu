@@ -845,7 +845,8 @@ sq_status_t launch_route(const void* logits, int dtype, int64_t T, int E, int64_
                                 : (threads == 256 ? route_kernel<LPT, EPL, 256, true> : route_kernel<LPT, EPL, BIG, true>);
     const int staged = chunk * k <= RT_STAGED;
     const int smem = ((2 * (threads / LPT) + 1) * E + 2 * threads + (staged ? 2 * RT_STAGED : 0)) * 4;
-    if (!ensure_dyn_smem(reinterpret_cast<const void*>(kern), smem)) return SQ_ERR_CUDA;
+    // The kernel's static shared memory, below 2 KB, counts towards the 48 KB that need no asking.
+    if (!ensure_dyn_smem(reinterpret_cast<const void*>(kern), smem > 46 * 1024 ? std::max(smem, 48 * 1024 + 16) : smem)) return SQ_ERR_CUDA;
     const cudaError_t err = launch_maybe_pdl(kern, dim3(static_cast<unsigned>(B)), dim3(static_cast<unsigned>(threads)), static_cast<size_t>(smem), s, a, chunk,
                                              staged, idsp, static_cast<float*>(gates), posp, hist, psum, cnt, off, rt, static_cast<float*>(loss));
     count_launch();

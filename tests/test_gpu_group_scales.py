@@ -53,7 +53,7 @@ SHAPES = [(1, 8, 8, 32), (1, 130, 40, 32), (3, 33, 72, 64), (1, 512, 512, 32), (
           (16, 2048, 512, 128), (17, 512, 512, 64), (31, 257, 640, 128), (33, 768, 1088, 64), (50, 520, 2048, 32), (64, 136, 576, 128),
           (65, 256, 512, 32), (100, 513, 832, 64), (129, 1024, 1024, 128), (200, 384, 320, 32), (257, 130, 4160, 128), (300, 1026, 512, 64),
           (1, 14336, 4096, 128), (6, 4096, 14336, 64), (1, 256, 28672, 32), (16, 128, 28672, 128), (1, 6, 65536, 128), (20, 128, 65536, 32),
-          (2, 64, 32, 32), (1, 2, 96, 64), (7, 66, 96, 128), (20, 40, 32, 128), (70, 50, 96, 32), (11, 2048, 2080, 64), (16, 8192, 4096, 128)]
+          (2, 64, 32, 32), (1, 2, 96, 64), (7, 66, 96, 128), (20, 40, 32, 128), (70, 50, 96, 32), (11, 2048, 2080, 64), (3, 129, 256, 64), (16, 33, 1024, 32), (16, 8192, 4096, 128)]
 
 
 @pytest.mark.parametrize("offset", [False, True])

@@ -86,6 +86,18 @@ def test_route(T, E, k, renorm, dtype):
     Routed(x, dtype, k, renorm, mask, ld=E if T % 3 else E + 5).check()
 
 
+@pytest.mark.parametrize("T,experts,k", [(200, range(17, 64), 2), (20, range(100, 420, 10), 3), (900, range(4, 17), 2), (300, range(257, 400, 7), 2)])
+def test_route_with_every_amount_of_shared_memory(T, experts, k):
+    """Around the 48 KB up to which a kernel need not ask for its shared memory, and on either side of every shape's border."""
+    rng = np.random.default_rng(T)
+    for E in experts:
+        x = rng.standard_normal((T, E))
+        r = Routed(x, "bf16" if E % 2 else "fp32", min(k, E), True)
+        got, want = r.read(), sbo.route(r.v, r.k, True)
+        for n in ("ids", "counts", "offsets", "pos"):
+            assert np.array_equal(got[n], want[n]), (E, n)
+
+
 def test_route_of_more_slots_than_stay_on_chip():
     """More than 4096 slots of a block: experts and ranks go through the outputs instead."""
     rng = np.random.default_rng(0)
