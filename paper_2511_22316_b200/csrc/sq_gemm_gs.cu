@@ -73,8 +73,9 @@ gs_simple_kernel(const GsArgs a) {
 // two kinds go to accumulators of their own, and behind each group, in fp32,
 //   sum += scale (lo - 8 sum(x) + hi / 16) + offset sum(x)      (in units of 2^-24),
 // with the group's sum of the tokens from an MMA with ones, once for all channels of the warp; -8 sum(x) is what lo begins with.  No
-// weight is rounded.  (With each
-// weight made fp16(code scale + offset) beforehand -- 13 operations for eight weights in place of 5 -- 1 x 4096 -> 14336 took 10.7 us.)
+// weight is rounded.  1 x 4096 -> 14336, groups of 128: 8.6 us, of which the loads alone take 4.8 (3.5 TB/s; 8192 -> 28672 26.9 us, 4.5
+// TB/s).  (With each weight made fp16(code scale + offset) beforehand, 13 operations for eight weights in place of 5, 10.7 us.)  What
+// bounds it: the instructions around the MMAs, some 5 cycles each for a warp, with four warps per scheduler.
 //
 // So that an MMA stays within a group of 32, 64 or 128, lane 4 g + t takes word t, words 2 t, 2 t + 1 or piece t (four words) of
 // the group: the MMA's order of k is whatever weights and tokens agree on.
@@ -122,13 +123,13 @@ __device__ __forceinline__ void lds_words(uint32_t a, uint32_t (&w)[W]) {
   else if constexpr (W == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(a) : "memory");
   else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(a) : "memory");
 }
-// Nibbles as subnormals: (w & mask) ^ sign.  The constants come in registers, see widen_consts.
 __device__ __forceinline__ void mma_f16_from(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1,
                                              float c0, float c1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%10,%11};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
 }
+// Nibbles as subnormals: (w & mask) ^ sign.  The constants come in registers, see widen_consts.
 struct NibbleConsts { uint32_t low, high; };
 __device__ __forceinline__ NibbleConsts nibble_consts() {
   const uint32_t one = gridDim.y;                        // 1, which the compiler does not know
