@@ -507,6 +507,20 @@ __device__ __forceinline__ uint32_t pack16(float a, float b, int dtype) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// What the slots of a group's token add to its logits' gradients, from the lanes that hold the slots to those that hold the logits,
+// through a row that is all zeros before and after.  The last barrier is for the next token, whose slot of the same expert
+// another lane may hold: its value must not be cleared by this one.  All lanes of the warp.
+template <int EPL>
+__device__ __forceinline__ void route_spread(float* row, bool put, int id, float add, int sub, float (&extra)[EPL]) {
+  if (put) row[id] = add;                            // the token's experts differ: no two lanes write one place
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) extra[i] = row[sub * EPL + i];
+  __syncwarp();
+  if (put) row[id] = 0.0f;
+  __syncwarp();
+}
+
 template <int LPT, int EPL>
 __global__ void __launch_bounds__(256)
 route_backward_kernel(const RouteArgs a, const int32_t* __restrict__ ids, const float* __restrict__ gates,
@@ -557,13 +571,7 @@ route_backward_kernel(const RouteArgs a, const int32_t* __restrict__ ids, const 
     float add = dg;
     if (a.renorm) add = g * (dg - group_sum<LPT>(g * dg));
     float extra[EPL];
-    const bool put = id >= 0 && id < E;              // the token's experts differ: no two lanes write one place
-    if (put) add_row[id] = add;
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) extra[i] = add_row[sub * EPL + i];
-    __syncwarp();
-    if (put) add_row[id] = 0.0f;
+    route_spread<EPL>(add_row, id >= 0 && id < E, id, add, sub, extra);
     if (!a.renorm) {
 #pragma unroll
       for (int i = 0; i < EPL; ++i) { d[i] += extra[i]; extra[i] = 0.0f; }
