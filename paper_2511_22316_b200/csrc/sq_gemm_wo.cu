@@ -443,10 +443,8 @@ wo_gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_const
 // channels.
 constexpr int WOD_CONV_GROUPS = 2;
 constexpr int WOD_CONV_WARPS = 4 * WOD_CONV_GROUPS;
-constexpr int WOD_T_WARP = 2 + WOD_CONV_WARPS + WO_EPI_WARPS;      // the token loads have a warp of their own
-constexpr int WOD_THREADS = (WOD_T_WARP + 1) * 32;
-constexpr int WOD_A_STAGES = 2;           // tensor-memory operand stages of 128 columns (256 fp16 channels)
-// accumulators: columns [0, 2 NT); operand ring: two stages of 128 columns from column max(128, 2 NT) on
+constexpr int WOD_A_STAGES = 3;           // tensor-memory operand stages at most; a converter group has one: 128 columns (256 fp16 channels)
+// accumulators: columns [0, 2 NT); operand ring: its stages from column max(128, 2 NT) on
 
 template <int NT, int ST, int SS>
 struct WoDecSmem {
@@ -474,7 +472,7 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
   // belong to the same tile -- channels [0, 128) and [128, 256) of it -- and every token block that
   // reaches shared memory feeds two MMAs instead of one.
   static_assert(CT == 1 || CT == 2, "one or two channel tiles per token tile");
-  static_assert(2 * NT + 128 * CG <= 512, "tensor-memory plan does not fit");
+  static_assert(CG <= WOD_A_STAGES && (2 * NT > 128 ? 2 * NT : 128) + 128 * CG <= 512, "tensor-memory plan does not fit");
   static_assert(SS % CG == 0, "a converter group meets every phase of its stages");
   constexpr int NBUF = 2 / CT;                           // accumulator sets that alternate between tiles
   constexpr int WOD_A_COL0 = 2 * NT > 128 ? 2 * NT : 128;
@@ -486,10 +484,9 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
   uint64_t* t_empty = t_full + ST;
   uint64_t* st_full = t_empty + ST;
   uint64_t* st_empty = st_full + SS;
-  __shared__ uint64_t a_bars[2 * CG];             // (the plan has room for two stages)
-  uint64_t* a_full = a_bars;
+  uint64_t* a_full = st_empty + SS;               // (barriers in static memory instead: 16 x 4096 -> 14336 11.9 -> 12.1 us)
   uint64_t* a_empty = a_full + CG;
-  uint64_t* tmem_full = st_empty + SS;            // [2]
+  uint64_t* tmem_full = a_empty + CG;             // [2]
   uint64_t* tmem_empty = tmem_full + 2;           // [2]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_TMEM);
 
