@@ -347,8 +347,9 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
         }
         if (n == 0) {
           cp_async_wait<L::DEPTH - 1>();
-          // (After a time-out nothing is requested any more, and what is on its way gets a little longer.)
-          ok = mbar_wait(&full[slot], phase, GS_FULL, ok ? limit : 65536u) && ok;
+          // (After a time-out nothing is requested any more, and what is on its way gets a little longer.  The lanes agree on it: what
+          // follows is the whole warp's.)
+          ok = __all_sync(0xFFFFFFFFu, mbar_wait(&full[slot], phase, GS_FULL, ok ? limit : 65536u) && ok) != 0;
           __syncwarp();                              // the other lanes' scales
         }
         // Experts: two blocks of channels side by side, as all tiles have four (a dense tile may have three: 26.9 us, and 30.2 in twos,

@@ -54,3 +54,42 @@ int main() {
     want = [0.0] * 96
     want[5], want[32 + 5] = 2.0, 3.0
     assert got == want
+
+
+def test_a_warp_of_the_stream_agrees_on_a_landing():
+    """One lane runs out of its wait for a landing that the others see: all go on alike (what follows has barriers of the whole warp)."""
+    src = source("sq_gemm_gs.cu")
+    start = src.index("cp_async_wait<L::DEPTH - 1>();")
+    piece = src[start:src.index("__syncwarp();", start)]
+    rows = run(WARP + """
+struct L { static constexpr int DEPTH = 4; };
+enum { GS_FULL = 112 };
+template <int N> void cp_async_wait() {}
+int votes[LANES];
+int __all_sync(unsigned, int v) {
+  votes[lane] = v;
+  barrier.wait();
+  int all = 1;
+  for (int i = 0; i < LANES; ++i) all &= votes[i] != 0;
+  barrier.wait();
+  return all;
+}
+int late = -1;
+bool mbar_wait(uint64_t*, uint32_t, uint32_t, uint32_t) { return lane != late; }
+volatile int got[2][32];
+int main() {
+  for (int t = 0; t < 2; ++t) {
+    late = t == 0 ? -1 : 7;
+    warp([t] {
+      uint64_t full[4] = {};
+      int slot = 0;
+      uint32_t phase = 0, limit = 100;
+      bool ok = true;
+      """ + piece + """
+      got[t][lane] = ok;
+    });
+  }
+  for (int t = 0; t < 2; ++t)
+    for (int i = 0; i < 32; ++i) printf("%d\\n", got[t][i]);
+}""")
+    assert [int(r[0]) for r in rows] == [1] * 32 + [0] * 32
