@@ -68,14 +68,18 @@ gs_simple_kernel(const GsArgs a) {
 // and it runs on from tile to tile.  The tokens come straight from L2 into the MMA's layout, eight rows ahead: each warp needs
 // another part of K.  (With 16-byte asynchronous copies in place of TMA a step of 16 x 128 weights took 169 instructions.)
 //
-// A nibble is not widened at all: masked out of its word it IS the fp16 subnormal v 2^-24 (bits 0 to 3) or v 2^-20 (bits 4 to 7), v =
-// code + 8, which the MMA multiplies exactly.  One shift by 8 and four logic operations make eight weights.  Products with the
-// two kinds go to accumulators of their own, and behind each group, in fp32,
-//   sum += scale (lo - 8 sum(x) + hi / 16) + offset sum(x)      (in units of 2^-24),
-// with the group's sum of the tokens from an MMA with ones, once for all channels of the warp; -8 sum(x) is what lo begins with.  No
-// weight is rounded.  1 x 4096 -> 14336, groups of 128: 8.6 us, of which the loads alone take 4.8 (3.5 TB/s; 8192 -> 28672 26.9 us, 4.5
-// TB/s).  (With each weight made fp16(code scale + offset) beforehand, 13 operations for eight weights in place of 5, 10.7 us.)  What
-// bounds it: the instructions around the MMAs, some 5 cycles each for a warp, with four warps per scheduler.
+// The MMA multiplies the codes themselves, widened to fp16 exactly (widen_word: nine operations for eight weights); the pairs that
+// the widening makes of low and of high bits go to accumulators of their own, two chains, and behind each group, in fp32,
+//   sum += scale (lo + hi) + offset sum(x),
+// with the group's sum of the tokens, where there are offsets, from an MMA with ones, once for all channels of the warp.  No weight is
+// rounded, and a code of zero adds nothing, whatever its token.  (Masked out of its word a nibble is an fp16 subnormal, code + 8,
+// that the MMA would take as it is, five operations in place of nine; but 8 sum(x) has to come off again, whose rounding showed where
+// a token is large and its code zero, and the chain for sum(x) stands before all others: groups of 128, 1 x 8192 -> 28672 26.7 us and 27.2
+// with the codes, 1 x 4096 -> 14336 8.8 both, 1 x 4096 -> 4096 5.6 and 4.7; 8 x 4096 -> 14336, groups of 64, 10.5 and 9.5.)  With
+// each weight made fp16(code scale + offset) beforehand, 1 x 4096 -> 14336 took 10.7 us.
+//
+// 1 x 4096 -> 14336 in 8.8 us is 3.4 TB/s, 1 x 8192 -> 28672 in 27.2 us 4.5 TB/s (graph replays): by the two some 2.6 us of a call are its
+// start and end, and the rest runs at 4.9 TB/s, 75 % of the copy rate.
 //
 // So that an MMA stays within a group of 32, 64 or 128, lane 4 g + t takes word t, words 2 t, 2 t + 1 or piece t (four words) of
 // the group: the MMA's order of k is whatever weights and tokens agree on.
@@ -111,7 +115,7 @@ __device__ __forceinline__ float lds_half(uint32_t a) {
   asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
   return __half2float(__ushort_as_half(v));
 }
-// D = A B, or A B + (c0, c1) in both halves of the rows: sums that begin.
+// D = A B: sums that begin.
 __device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
@@ -122,28 +126,6 @@ __device__ __forceinline__ void lds_words(uint32_t a, uint32_t (&w)[W]) {
   if constexpr (W == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(a) : "memory");
   else if constexpr (W == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(a) : "memory");
   else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(a) : "memory");
-}
-__device__ __forceinline__ void mma_f16_from(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1,
-                                             float c0, float c1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%10,%11};"
-      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
-}
-// Nibbles as subnormals: (w & mask) ^ sign.  The constants come in registers, see widen_consts.
-struct NibbleConsts { uint32_t low, high; };
-__device__ __forceinline__ NibbleConsts nibble_consts() {
-  const uint32_t one = gridDim.y;                        // 1, which the compiler does not know
-  return {0x00080007u + one, 0x0080007Fu + one};
-}
-__device__ __forceinline__ uint32_t low_nibbles(uint32_t w, const NibbleConsts& k) {
-  uint32_t x;
-  asm("lop3.b32 %0, %1, 0x000F000F, %2, 0x6a;" : "=r"(x) : "r"(w), "r"(k.low));
-  return x;
-}
-__device__ __forceinline__ uint32_t high_nibbles(uint32_t w, const NibbleConsts& k) {
-  uint32_t x;
-  asm("lop3.b32 %0, %1, 0x00F000F0, %2, 0x6a;" : "=r"(x) : "r"(w), "r"(k.high));
-  return x;
 }
 
 __device__ const uint4 g_zero_words[4] = {};
@@ -304,7 +286,7 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
   };
   fetch(0);
 
-  const NibbleConsts nk = nibble_consts();
+  const WidenConsts wk = widen_consts();
   const uint32_t ones = 0x3C003C00u;
   int slot = 0;
   uint32_t phase = 0;
@@ -314,7 +296,7 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
     const int size = EXPERTS ? RB : dense_size(tile, my_tiles - tl);
     const int row0 = EXPERTS ? (tile - chunk * ctiles) * R : 16 * tile, rows = min(EXPERTS ? R : 16 * size, N - row0);
     tile += EXPERTS ? ncl : size;
-    float acc[RB][NT][4];                            // in units of 2^-24
+    float acc[RB][NT][4];
 #pragma unroll
     for (int b = 0; b < RB; ++b)
 #pragma unroll
@@ -323,7 +305,7 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
         for (int e = 0; e < 4; ++e) acc[b][n][e] = 0.0f;
     for (int i = 0; i < cw; ++i) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {                 // (16 rows: the nibbles are masked out twice, which costs less than 32 more registers)
+      for (int n = 0; n < NT; ++n) {                 // (16 rows: the codes are widened twice, which costs less than 32 more registers)
         // Channel pairs (0, 1) and (4, 5) of each word, then (2, 3) and (6, 7): as the MMAs take them.
         uint2 xl[4], xh[4];
         float2 sx[CHUNKS];
@@ -333,17 +315,19 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
           xh[j] = make_uint2(xn[j].y, xn[j].w);
         }
         fetch((n + 1) % NT);
+        if constexpr (BIAS) {
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-          float d[4];
+          for (int c = 0; c < CHUNKS; ++c) {
+            float d[4];
 #pragma unroll
-          for (int j = 0; j < WPL; ++j) {
-            const uint2 vl = xl[c * WPL + j], vh = xh[c * WPL + j];
-            if (j == 0) mma_f16_first(d, ones, ones, ones, ones, vl.x, vl.y);
-            else mma_f16(d, ones, ones, ones, ones, vl.x, vl.y);
-            mma_f16(d, ones, ones, ones, ones, vh.x, vh.y);
+            for (int j = 0; j < WPL; ++j) {
+              const uint2 vl = xl[c * WPL + j], vh = xh[c * WPL + j];
+              if (j == 0) mma_f16_first(d, ones, ones, ones, ones, vl.x, vl.y);
+              else mma_f16(d, ones, ones, ones, ones, vl.x, vl.y);
+              mma_f16(d, ones, ones, ones, ones, vh.x, vh.y);
+            }
+            sx[c] = make_float2(d[0], d[1]);
           }
-          sx[c] = make_float2(d[0] * 0x1p-24f, d[1] * 0x1p-24f);
         }
         if (n == 0) {
           cp_async_wait<L::DEPTH - 1>();
@@ -380,15 +364,13 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
               const uint2 p = xl[c * WPL + j], q = xh[c * WPL + j];
 #pragma unroll
               for (int b = 0; b < PB; ++b) {
-                const uint32_t uw = u[b][j], vw = v[b][j], u8 = uw >> 8, v8 = vw >> 8;
-                const uint32_t ul = low_nibbles(uw, nk), vl = low_nibbles(vw, nk), ul8 = low_nibbles(u8, nk), vl8 = low_nibbles(v8, nk);
-                const uint32_t uh = high_nibbles(uw, nk), vh = high_nibbles(vw, nk), uh8 = high_nibbles(u8, nk), vh8 = high_nibbles(v8, nk);
-                if (j == 0) {                        // -8 sum(x): v is code + 8
-                  mma_f16_from(lo[b], ul, vl, ul8, vl8, p.x, p.y, -8.0f * sx[c].x, -8.0f * sx[c].y);
-                  mma_f16_first(hi[b], uh, vh, uh8, vh8, q.x, q.y);
+                const uint4 uc = widen_word(u[b][j], wk), vc = widen_word(v[b][j], wk);
+                if (j == 0) {
+                  mma_f16_first(lo[b], uc.x, vc.x, uc.z, vc.z, p.x, p.y);
+                  mma_f16_first(hi[b], uc.y, vc.y, uc.w, vc.w, q.x, q.y);
                 } else {
-                  mma_f16(lo[b], ul, vl, ul8, vl8, p.x, p.y);
-                  mma_f16(hi[b], uh, vh, uh8, vh8, q.x, q.y);
+                  mma_f16(lo[b], uc.x, vc.x, uc.z, vc.z, p.x, p.y);
+                  mma_f16(hi[b], uc.y, vc.y, uc.w, vc.w, q.x, q.y);
                 }
               }
             }
@@ -397,7 +379,7 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
 #pragma unroll
               for (int e = 0; e < 4; ++e) {          // e & 1: token 2 t or 2 t + 1, e >> 1: channel g or g + 8
                 float& sum = acc[b0 + b][n][e];
-                sum = fmaf(e < 2 ? s[b].x : s[b].y, fmaf(hi[b][e], 0.0625f, lo[b][e]), sum);
+                sum = fmaf(e < 2 ? s[b].x : s[b].y, lo[b][e] + hi[b][e], sum);
                 if (BIAS) sum = fmaf(e < 2 ? o[b].x : o[b].y, (e & 1) ? sx[c].y : sx[c].x, sum);
               }
           }
@@ -417,10 +399,10 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         float* p = mine + (8 * n + 2 * t) * L::PITCH + 16 * b + g;
-        p[0] = acc[b][n][0] * 0x1p24f;
-        p[L::PITCH] = acc[b][n][1] * 0x1p24f;
-        p[8] = acc[b][n][2] * 0x1p24f;
-        p[L::PITCH + 8] = acc[b][n][3] * 0x1p24f;
+        p[0] = acc[b][n][0];
+        p[L::PITCH] = acc[b][n][1];
+        p[8] = acc[b][n][2];
+        p[L::PITCH + 8] = acc[b][n][3];
       }
     __syncthreads();
     long long r0 = 0, r1 = a.M;
