@@ -565,7 +565,7 @@ route_backward_kernel(const RouteArgs a, const int32_t* __restrict__ ids, const 
         g = gates[t * k + sub];
       }
     }
-    route_softmax<LPT, EPL>(x, p, m, inv);
+    const bool counts_in = route_softmax<LPT, EPL>(x, p, m, inv);
 #pragma unroll
     for (int i = 0; i < EPL; ++i) d[i] = c[i];
     float add = dg;
@@ -581,7 +581,7 @@ route_backward_kernel(const RouteArgs a, const int32_t* __restrict__ ids, const 
     for (int i = 0; i < EPL; ++i) dot += p[i] * d[i];
     dot = group_sum<LPT>(dot);
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) d[i] = p[i] * (d[i] - dot) + extra[i];
+    for (int i = 0; i < EPL; ++i) d[i] = counts_in ? p[i] * (d[i] - dot) + extra[i] : 0.0f;      // (a loss that overflowed times p = 0)
     if (!in) continue;
     const int e0 = sub * EPL;
     if (a.dtype == SQ_F32) {

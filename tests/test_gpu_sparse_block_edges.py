@@ -2,6 +2,8 @@
 import numpy as np
 import pytest
 
+from gpu_util import Guarded, dev
+from paper_2511_22316_b200 import binding as sq
 from test_gpu_sparse_block import Backward, Routed
 
 pytestmark = pytest.mark.gpu
@@ -15,3 +17,23 @@ def test_gradient_of_more_tokens_than_lanes_that_take_them(T, E, k, renorm):
     rng = np.random.default_rng(T)
     x = rng.standard_normal((T, E)) + np.where(np.arange(E) < k + 1, 4.0, 0.0)
     Backward(Routed(x, "fp32", k, renorm, rng.random(T) < 0.9), rng).check()
+
+
+@pytest.mark.parametrize("dloss", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("T,E", [(6, 8), (300, 40)])
+def test_tokens_that_do_not_count_have_no_gradient_even_of_an_overflown_loss(T, E, renorm, dloss):
+    rng = np.random.default_rng(T)
+    x = rng.standard_normal((T, E)).astype(np.float32)
+    x[1] = -np.inf
+    x[2] = np.nan
+    mask = np.ones(T)
+    mask[4:] = rng.random(T - 4) < 0.5
+    mask[3], mask[4] = 0, 1
+    r = Routed(x, "fp32", 2, renorm, mask)
+    out, g = Guarded(T * E * 4), r.g
+    sq.sq_route_backward(r.t, r.code, T, E, E, 2, sq.SQ_ROUTE_RENORM if renorm else 0, r.mask, g["ids"], g["gates"], g["counts"], None,
+                         dev(np.array([dloss], np.float32)), out, E)
+    got = out.numpy(np.float32, (T, E))
+    counted = (mask > 0) & (np.arange(T) != 1) & (np.arange(T) != 2)
+    assert not got[~counted].any() and not np.isfinite(got[counted]).all(1).any()
