@@ -888,7 +888,7 @@ sq_status_t sq_combine_backward(const void* dout, const void* Y, int64_t M, cons
                                 int64_t N, void* dY_or_null, void* dgates_or_null, void* stream) {
   sq_status_t st = check_combine_args(M, T, k, N);
   if (st != SQ_OK || T == 0 || (N == 0 && !dgates_or_null)) return st;
-  if (!dout || (!Y && M > 0) || !pos || !gates || (dY_or_null && (dY_or_null == Y || dY_or_null == dout))) return SQ_ERR_INVALID_ARG;
+  if ((!dout && N > 0) || (!Y && M > 0 && N > 0) || !pos || !gates || (dY_or_null && (dY_or_null == Y || dY_or_null == dout))) return SQ_ERR_INVALID_ARG;
   if (!all_aligned({dout, Y, pos, gates, dY_or_null, dgates_or_null})) return SQ_ERR_ALIGN;
   if (!dY_or_null && !dgates_or_null) return SQ_OK;
   return sq::launch_combine_backward(dout, Y, M, pos, gates, T, k, N, dY_or_null, dgates_or_null, static_cast<cudaStream_t>(stream));

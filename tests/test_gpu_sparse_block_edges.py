@@ -37,3 +37,12 @@ def test_tokens_that_do_not_count_have_no_gradient_even_of_an_overflown_loss(T, 
     got = out.numpy(np.float32, (T, E))
     counted = (mask > 0) & (np.arange(T) != 1) & (np.arange(T) != 2)
     assert not got[~counted].any() and not np.isfinite(got[counted]).all(1).any()
+
+
+def test_gradient_of_a_combination_without_channels():
+    """Rows of no channels need no memory behind them; the gates' gradients are sums of nothing."""
+    dg = Guarded(5 * 2 * 4)
+    sq.sq_combine_backward(None, None, 9, dev(np.zeros((5, 2), np.int32)), dev(np.ones((5, 2), np.float32)), 5, 2, 0, None, dg)
+    got = dg.numpy(np.uint32, (5, 2))
+    dg.check()
+    assert not got.any()
