@@ -30,6 +30,7 @@ namespace {
 constexpr int RT_MAX_BLOCKS = 148;                   // the second kernel reads every block's counts, five to a lane
 constexpr int RT_STAGED = 4096;                      // slots of a block whose expert and rank stay in shared memory
 constexpr int RT_CHUNKS = 1;                         // blocks of the first kernel that one of the second finishes
+constexpr int RT_FLUSH = 64;                         // tokens whose probabilities are added up in a register before they join the sums
 constexpr uint32_t RT_KEY_NINF = 0x007FFFFFu;        // route_key(-inf): not above it is not usable
 constexpr float RT_NINF = -__builtin_huge_valf();
 
@@ -274,8 +275,8 @@ route_kernel(const RouteArgs a, long long chunk, int staged, int32_t* __restrict
   griddep_wait();                                    // the logits come from, and the outputs may be read by, the kernel before
 
   const long long first = blockIdx.x * chunk, last = first + chunk < a.T ? first + chunk : a.T;
-  const long long run = (chunk + GROUPS - 1) / GROUPS;
-  const long long t0 = first + grp * run, t1 = t0 + run < last ? t0 + run : last;
+  const int run = static_cast<int>((chunk + GROUPS - 1) / GROUPS);         // (a 148th of 2^31 tokens)
+  const long long t0 = first + static_cast<long long>(grp) * run, t1 = t0 + run < last ? t0 + run : last;
   int* my_cnt = cnt + grp * E;
   float acc[EPL], x[EPL], next[EPL];
   bool next_live = false;
@@ -287,43 +288,53 @@ route_kernel(const RouteArgs a, long long chunk, int staged, int32_t* __restrict
     next_live = a.mask == nullptr || a.mask[t] != 0;
   };
   if (t0 < t1) load(t0);
-  for (long long it = 0; it < run; ++it) {           // every group of a warp: the shuffles below are the warp's
-    const long long t = t0 + it;
-    const bool in = t < t1;
+  // A run's probabilities are added up by 64 tokens at a time, so that no sum has more than 64 and a 64th of the run's roundings.
+  int it = 0;
+  do {
+    const bool begun = it > 0;
+    const int end = min(it + RT_FLUSH, run);
+    for (; it < end; ++it) {                         // every group of a warp: the shuffles below are the warp's
+      const long long t = t0 + it;
+      const bool in = t < t1;
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) x[i] = in && next_live ? next[i] : RT_NINF;
-    if (t + 1 < t1) load(t + 1);
-    float p[EPL], m, inv;
-    live += route_softmax<LPT, EPL>(x, p, m, inv) ? 1 : 0;
+      for (int i = 0; i < EPL; ++i) x[i] = in && next_live ? next[i] : RT_NINF;
+      if (t + 1 < t1) load(t + 1);
+      float p[EPL], m, inv;
+      live += route_softmax<LPT, EPL>(x, p, m, inv) ? 1 : 0;
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) acc[i] += p[i];
-    int my_id;
-    float my_x;
-    route_select<LPT, EPL, KEY16>(x, sub, k, my_id, my_x);
-    if (sub >= k) my_id = -1;
-    const float ev = my_id >= 0 ? route_exp(my_x, m) : 0.0f;
-    const float scale = a.renorm ? 1.0f / group_sum<LPT>(ev) : inv;
-    if (in && sub < k) {
-      const long long o = t * k + sub;
-      ids[o] = my_id;
-      gates[o] = my_id >= 0 ? ev * scale : 0.0f;
-      int r = -1;
-      if (my_id >= 0) {                              // the token's experts differ: no two lanes share a counter
-        r = my_cnt[my_id];
-        my_cnt[my_id] = r + 1;
+      for (int i = 0; i < EPL; ++i) acc[i] += p[i];
+      int my_id;
+      float my_x;
+      route_select<LPT, EPL, KEY16>(x, sub, k, my_id, my_x);
+      if (sub >= k) my_id = -1;
+      const float ev = my_id >= 0 ? route_exp(my_x, m) : 0.0f;
+      const float scale = a.renorm ? 1.0f / group_sum<LPT>(ev) : inv;
+      if (in && sub < k) {
+        const long long o = t * k + sub;
+        ids[o] = my_id;
+        gates[o] = my_id >= 0 ? ev * scale : 0.0f;
+        int r = -1;
+        if (my_id >= 0) {                              // the token's experts differ: no two lanes share a counter
+          r = my_cnt[my_id];
+          my_cnt[my_id] = r + 1;
+        }
+        if (staged) {
+          slot_id[o - first * k] = my_id;
+          slot_rank[o - first * k] = r;
+        } else {
+          pos[o] = r;                                  // within the group, for now
+        }
       }
-      if (staged) {
-        slot_id[o - first * k] = my_id;
-        slot_rank[o - first * k] = r;
-      } else {
-        pos[o] = r;                                  // within the group, for now
-      }
+      __syncwarp();
     }
-    __syncwarp();
-  }
 #pragma unroll
-  for (int i = 0; i < EPL; ++i)
-    if (sub * EPL + i < E) ps[grp * E + sub * EPL + i] = acc[i];
+    for (int i = 0; i < EPL; ++i)
+      if (sub * EPL + i < E) {
+        float* sum = ps + grp * E + sub * EPL + i;
+        *sum = begun ? *sum + acc[i] : acc[i];
+        acc[i] = 0.0f;
+      }
+  } while (it < run);
   if (sub == 0) live_of[grp] = live;
   __syncthreads();
 

@@ -46,3 +46,21 @@ def test_gradient_of_a_combination_without_channels():
     got = dg.numpy(np.uint32, (5, 2))
     dg.check()
     assert not got.any()
+
+
+@pytest.mark.parametrize("T,E", [(4000000, 49), (2000000, 60), (70000, 7)])
+def test_loss_of_many_tokens(T, E):
+    """All logits alike: every token has 1 / E of every expert and goes to the first, so the loss is 1.  Each addition of equal numbers
+    is off to the same side, which a plain sum of a run of tokens shows."""
+    import torch
+    x = torch.zeros(T, E, dtype=torch.float16, device="cuda")
+    i32 = lambda *n: torch.empty(*n, dtype=torch.int32, device="cuda")
+    ids, gates, pos, row_token, counts, offsets = i32(T, 1), i32(T, 1), i32(T, 1), i32(T), i32(E + 1), i32(E + 1)
+    loss = torch.empty(1, dtype=torch.float32, device="cuda")
+    nb = sq.sq_route_workspace_bytes(T, E)
+    sq.sq_route(x, sq.SQ_F16, T, E, E, 1, 0, None, ids, gates, counts, offsets, row_token, pos, loss, torch.empty(nb, dtype=torch.uint8, device="cuda"), nb)
+    assert counts.tolist() == [T] + [0] * (E - 1) + [T] and offsets.tolist() == [0] + [T] * E
+    run = -(-(-(-T // 148)) // 32)
+    # 1 / E once; 64 additions in a register, one for each 64 tokens, at most 24 over the groups of a block, 10 over the blocks; the result
+    roundings = 1 + 64 + run // 64 + 1 + 24 + 10 + 1
+    assert abs(loss.item() - 1) <= roundings * 2.0 ** -24 * (1 + 2.0 ** -10)
