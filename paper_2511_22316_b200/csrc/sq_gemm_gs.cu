@@ -100,7 +100,7 @@ struct GsStream {
   static constexpr int OFF_PART = GS_WARPS * RING;
   static constexpr int OFF_BAR = OFF_PART + GS_WARPS * 4 * PART;
   static constexpr int BYTES = OFF_BAR + GS_WARPS * DEPTH * 8 + 512;                // slack for the alignment
-  static_assert(BYTES <= 112 * 1024, "two blocks to an SM");
+  static_assert(BYTES + (1025 + 33) * 4 <= 113 * 1024, "two blocks to an SM, with the experts' chunks and the scan in static memory");
 };
 enum GsSite : uint32_t { GS_FULL = 112 };
 
@@ -132,9 +132,9 @@ __device__ const uint4 g_zero_words[4] = {};
 
 template <int RB, int NT, int GROUP, bool BIAS, bool EXPERTS>
 __global__ void __launch_bounds__(GS_THREADS, 2)
-gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ GsArgs a, int R, int splits) {
+gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ GsArgs a, int splits) {
   using L = GsStream<RB, NT, GROUP>;
-  constexpr int CHUNKS = L::CHUNKS, WPL = L::WPL;
+  constexpr int CHUNKS = L::CHUNKS, WPL = L::WPL, R = L::ROWS;
   griddep_launch_dependents();
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 511) & ~uintptr_t(511));
@@ -560,7 +560,7 @@ sq_status_t launch_stream_as(const GsArgs& a, int splits, int grid, cudaStream_t
           CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return SQ_ERR_CUDA;
   const cudaError_t err = launch_cluster_maybe_pdl(kern, dim3(static_cast<unsigned>(grid)), dim3(GS_THREADS), static_cast<size_t>(L::BYTES),
-                                                   s, static_cast<unsigned>(splits), mw, a, 16 * RB, splits);
+                                                   s, static_cast<unsigned>(splits), mw, a, splits);
   count_launch();
   return err == cudaSuccess ? SQ_OK : SQ_ERR_CUDA;
 }

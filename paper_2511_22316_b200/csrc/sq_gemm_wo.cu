@@ -1369,7 +1369,7 @@ template <int SS, class X = WoPlain>
 sq_status_t launch_wo_pair(const void* Z16, const void* Wq, const void* sw, int M, int N, int K, void* Y, cudaStream_t s,
                            const X& x = X(), int weight_rows = 0, int tile_m = 0) {
   using L = WoPairSmem<SS>;
-  static_assert(L::DYN_BYTES <= 227 * 1024, "shared-memory plan does not fit");
+  static_assert(L::DYN_BYTES + (X::EXPERTS ? (1025 + 33) * 4 : 4) <= 227 * 1024, "shared-memory plan does not fit");      // and what is static
   EncodeTiledFn enc = get_encode_fn();
   if (!enc) return SQ_ERR_CUDA;
   CUtensorMap mz, mw;

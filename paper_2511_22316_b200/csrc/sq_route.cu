@@ -29,7 +29,6 @@ namespace {
 
 constexpr int RT_MAX_BLOCKS = 148;                   // the second kernel reads every block's counts, five to a lane
 constexpr int RT_STAGED = 4096;                      // slots of a block whose expert and rank stay in shared memory
-constexpr int RT_CHUNKS = 1;                         // blocks of the first kernel that one of the second finishes
 constexpr int RT_FLUSH = 64;                         // tokens whose probabilities are added up in a register before they join the sums
 constexpr uint32_t RT_KEY_NINF = 0x007FFFFFu;        // route_key(-inf): not above it is not usable
 constexpr float RT_NINF = -__builtin_huge_valf();
@@ -419,8 +418,8 @@ route_kernel(const RouteArgs a, long long chunk, int staged, int32_t* __restrict
   }
 }
 
-// Blocks 0 .. gridDim.x - 2: the final rows of RT_CHUNKS blocks' tokens.  The last block: counts, offsets and the loss.
-// Shared memory: base [RT_CHUNKS][E], total [E], sum of p [E].
+// Blocks 0 .. B - 1: the final rows of the tokens of a block of the first kernel.  The last block: counts, offsets and the loss.
+// Shared memory: base [E], total [E], sum of p [E].
 __global__ void __launch_bounds__(1024)
 route_finish_kernel(int B, int E, int k, long long T, long long chunk, const int32_t* __restrict__ hist,
                     const float* __restrict__ psum, const int32_t* __restrict__ ids, int32_t* pos, int32_t* __restrict__ counts,
@@ -428,14 +427,15 @@ route_finish_kernel(int B, int E, int k, long long T, long long chunk, const int
   griddep_launch_dependents();
   extern __shared__ __align__(16) unsigned char rt_smem[];
   int* base = reinterpret_cast<int*>(rt_smem);
-  int* total = base + RT_CHUNKS * E;
+  int* total = base + E;
   float* prob = reinterpret_cast<float*>(total + E);
   __shared__ int warp_sums[33];
   __shared__ double sums[32];
   griddep_wait();
 
-  const bool summing = blockIdx.x + 1 == gridDim.x;
-  const int c0 = summing ? B : blockIdx.x * RT_CHUNKS, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int mine = static_cast<int>(blockIdx.x);     // B: the sums
+  const bool summing = mine == B;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr int PER = (RT_MAX_BLOCKS + 31) / 32;
   for (int e = warp; e < E; e += 32) {               // a warp takes an expert: every block's count of it
     int v[PER];
@@ -446,27 +446,21 @@ route_finish_kernel(int B, int E, int k, long long T, long long chunk, const int
       v[i] = b < B ? hist[static_cast<size_t>(e) * B + b] : 0;
       q[i] = summing && b < B ? psum[static_cast<size_t>(e) * B + b] : 0.0f;
     }
-    int all = 0, s[RT_CHUNKS];
+    int all = 0, before = 0;
     float p = 0.0f;
-#pragma unroll
-    for (int c = 0; c < RT_CHUNKS; ++c) s[c] = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       all += v[i];
       p += q[i];
-#pragma unroll
-      for (int c = 0; c < RT_CHUNKS; ++c) s[c] += lane + 32 * i < c0 + c ? v[i] : 0;
+      before += lane + 32 * i < mine ? v[i] : 0;
     }
     all = __reduce_add_sync(0xFFFFFFFFu, all);
     if (summing) {
       p = group_sum<32>(p);
       if (lane == 0) prob[e] = p;
     } else {
-#pragma unroll
-      for (int c = 0; c < RT_CHUNKS; ++c) {
-        s[c] = __reduce_add_sync(0xFFFFFFFFu, s[c]);
-        if (lane == c) base[c * E + e] = s[c];
-      }
+      before = __reduce_add_sync(0xFFFFFFFFu, before);
+      if (lane == 0) base[e] = before;
     }
     if (lane == 0) total[e] = all;
   }
@@ -492,19 +486,15 @@ route_finish_kernel(int B, int E, int k, long long T, long long chunk, const int
     }
     return;
   }
-  if (e < E)
-#pragma unroll
-    for (int c = 0; c < RT_CHUNKS; ++c) base[c * E + e] += off;
+  if (e < E) base[e] += off;
   __syncthreads();
-  for (int c = 0; c < RT_CHUNKS && c0 + c < B; ++c) {
-    const long long first = (c0 + c) * chunk, last = first + chunk < T ? first + chunk : T;
-    for (long long i = first * k + threadIdx.x; i < last * k; i += blockDim.x) {
-      const int id = ids[i];
-      if (id >= 0) {
-        const int r = pos[i] + base[c * E + id];
-        pos[i] = r;
-        row_token[r] = static_cast<int32_t>(first + static_cast<unsigned>(i - first * k) / static_cast<unsigned>(k));
-      }
+  const long long first = mine * chunk, last = first + chunk < T ? first + chunk : T;
+  for (long long i = first * k + threadIdx.x; i < last * k; i += blockDim.x) {
+    const int id = ids[i];
+    if (id >= 0) {
+      const int r = pos[i] + base[id];
+      pos[i] = r;
+      row_token[r] = static_cast<int32_t>(first + static_cast<unsigned>(i - first * k) / static_cast<unsigned>(k));
     }
   }
 }
@@ -873,8 +863,8 @@ sq_status_t launch_route(const void* logits, int dtype, int64_t T, int E, int64_
     return err == cudaSuccess ? SQ_OK : SQ_ERR_CUDA;
   });
   if (st != SQ_OK || B == 1) return st;
-  const int smem = (RT_CHUNKS + 2) * E * 4;
-  const cudaError_t err = launch_dependent(route_finish_kernel, dim3(static_cast<unsigned>((B + RT_CHUNKS - 1) / RT_CHUNKS + 1)), dim3(1024), static_cast<size_t>(smem), s, B,
+  const int smem = 3 * E * 4;
+  const cudaError_t err = launch_dependent(route_finish_kernel, dim3(static_cast<unsigned>(B + 1)), dim3(1024), static_cast<size_t>(smem), s, B,
                                            E, k, static_cast<long long>(T), chunk, static_cast<const int32_t*>(hist),
                                            static_cast<const float*>(psum), static_cast<const int32_t*>(idsp), posp, cnt, off, rt,
                                            static_cast<float*>(loss));
