@@ -2,7 +2,9 @@
 import numpy as np
 import pytest
 
+from gpu_util import Guarded, dev
 from oracle import sparse_block_oracle as sbo
+from paper_2511_22316_b200 import binding as sq
 from test_gpu_group_scales import U16, U32, check, check_grouped, make_weights, run_dense, run_grouped
 
 pytestmark = pytest.mark.gpu
@@ -49,3 +51,52 @@ def test_large_tokens_leave_no_trace_where_the_code_is_zero(M, group):
     ws = [(codes, sg, None)] * 4
     Y = run_grouped(np.resize(Z, (4 * per, 2048)), ws, None, np.arange(5) * per, 4 * per, group)
     assert np.all(np.abs(Y - np.resize(exact, Y.shape)) <= np.resize(tol, Y.shape))
+
+
+@pytest.mark.parametrize("E,rows", [(257, 3), (300, 9), (609, 2), (700, 10), (1024, 1), (1024, 9)])
+def test_more_experts_than_a_block_has_threads(E, rows):
+    """Up to 1024 experts, with some 8 rows each (the stream, 256 threads a block) or more (CTA pairs, 608 threads)."""
+    rng = np.random.default_rng(E + rows)
+    counts = rng.multinomial(rows * E, rng.dirichlet(np.full(E, 0.5)))
+    counts[[0, 1, E - 1]] = 0, 2, 3
+    offsets = np.concatenate([[0], np.cumsum(counts)])
+    M = int(offsets[-1]) + 5
+    ws = [make_weights(rng, 66, 96, 32, True) for _ in range(E)]
+    Z = rng.standard_normal((50, 96)).astype(np.float16)
+    row_token = rng.integers(0, 50, M)
+    check_grouped(run_grouped(Z, ws, row_token, offsets, M, 32), Z, ws, row_token, offsets, 32)
+
+
+@pytest.mark.parametrize("M", [1, 9, 17, 33, 65, 130, 700])
+@pytest.mark.parametrize("N,offset", [(200, True), (77, False)])
+def test_layer_in_front_of_every_kernel(M, N, offset):
+    """The rotation writes what the product behind it reads at once: every kernel as the rotation's dependent, twice in a row."""
+    import torch
+    n1, n2, group = 16, 32, 64
+    K = n1 * n2
+    rng = np.random.default_rng(M)
+    rot = sq.sq_build_rotation(rng.standard_normal((6, K)).astype(np.float32), n1, n2)
+    codes, sg, bg = make_weights(rng, N, K, group, offset)
+    w = sbo.weights(codes, sg, bg, group)
+    Wq, s, b = dev(sbo.pack_codes(codes)), dev(sg), None if bg is None else dev(bg)
+    nb = sq.sq_linear_wo_workspace_bytes(M, K)
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+    for X in rng.standard_normal((2, M, K)).astype(np.float16):
+        x, Y = dev(X), Guarded(M * N * 2)
+        sq.sq_linear_gs(rot, x, M, Wq, s, b, N, K, group, ws, nb, Y)
+        Z16 = torch.empty(M, K, dtype=torch.float16, device="cuda")
+        sq.sq_rotate_act_f16(rot, x, M, Z16)
+        assert sq.sq_last_device_status() == sq.SQ_OK
+        Y.check()
+        check(Y.numpy(np.float16, (M, N)), Z16.cpu().numpy(), w)
+    # the same as the layers of two experts, whose rows are the tokens twice, in another order
+    rows = np.concatenate([rng.permutation(M), rng.permutation(M)])
+    offsets = np.array([0, M // 3, 2 * M], np.int32)
+    nb = sq.sq_linear_gs_grouped_workspace_bytes(M, 2 * M, K)
+    ws, Y = torch.empty(nb, dtype=torch.uint8, device="cuda"), Guarded(2 * M * N * 2)
+    two = lambda t: None if t is None else torch.stack([t, t])
+    sq.sq_linear_gs_grouped(rot, x, M, dev(rows.astype(np.int32)), dev(offsets), 2, two(Wq), two(s), two(b), 2 * M, N, K, group, ws, nb, Y)
+    assert sq.sq_last_device_status() == sq.SQ_OK
+    Y.check()
+    check(Y.numpy(np.float16, (2 * M, N)), Z16.cpu().numpy()[rows], w)
+    rot.close()
