@@ -568,7 +568,7 @@ route_backward_kernel(const RouteArgs a, const int32_t* __restrict__ ids, const 
     }
     const bool counts_in = route_softmax<LPT, EPL>(x, p, m, inv);
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) d[i] = c[i];
+    for (int i = 0; i < EPL; ++i) d[i] = counts_in ? c[i] : 0.0f;         // (p = 0 times a loss that overflowed)
     float add = dg;
     if (a.renorm) add = g * (dg - group_sum<LPT>(g * dg));
     float extra[EPL];
@@ -582,7 +582,7 @@ route_backward_kernel(const RouteArgs a, const int32_t* __restrict__ ids, const 
     for (int i = 0; i < EPL; ++i) dot += p[i] * d[i];
     dot = group_sum<LPT>(dot);
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) d[i] = counts_in ? p[i] * (d[i] - dot) + extra[i] : 0.0f;      // (a loss that overflowed times p = 0)
+    for (int i = 0; i < EPL; ++i) d[i] = p[i] * (d[i] - dot) + extra[i];
     if (!in) continue;
     const int e0 = sub * EPL;
     if (a.dtype == SQ_F32) {
