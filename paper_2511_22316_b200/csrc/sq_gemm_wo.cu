@@ -484,9 +484,12 @@ wo_gemm_tmem_kernel(const __grid_constant__ CUtensorMap tmap_z, const __grid_con
   uint64_t* t_empty = t_full + ST;
   uint64_t* st_full = t_empty + ST;
   uint64_t* st_empty = st_full + SS;
-  uint64_t* a_full = st_empty + SS;               // (barriers in static memory instead: 16 x 4096 -> 14336 11.9 -> 12.1 us)
+  // The operand stages' barriers: in static memory with group scales (50 x 8192 -> 28672 45.9 -> 45.2 us), in the plan without (16 x 4096
+  // -> 14336 12.07 -> 11.89, 64 x 8192 -> 28672 47.5 -> 46.8).
+  __shared__ uint64_t gs_bars[X::GS ? 2 * CG : 1];
+  uint64_t* a_full = X::GS ? gs_bars : st_empty + SS;
   uint64_t* a_empty = a_full + CG;
-  uint64_t* tmem_full = a_empty + CG;             // [2]
+  uint64_t* tmem_full = st_empty + SS + 2 * CG;   // [2]
   uint64_t* tmem_empty = tmem_full + 2;           // [2]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_TMEM);
 
