@@ -336,52 +336,43 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
           ok = __all_sync(0xFFFFFFFFu, mbar_wait(&full[slot], phase, GS_FULL, ok ? limit : 65536u) && ok) != 0;
           __syncwarp();                              // the other lanes' scales
         }
-        // Experts: two blocks of channels side by side, as all tiles have four (a dense tile may have three: 26.9 us, and 30.2 in twos,
-        // for 1 x 8192 -> 28672).
-        constexpr int PB = EXPERTS ? 2 : 1;
+        // A tile of experts has all its blocks of channels but for an expert's last (what lies behind the channels is not stored), and
+        // without a way out of the loop the compiler mixes the blocks: 16 tokens on eight experts, 4096 -> 14336, groups of 128 55.7 -> 53.8
+        // us (two blocks side by side: 57.4); groups of 32 71.9 -> 71.1, with offsets 86.8 -> 84.6.  The other forms run out of registers by it: groups of 64 63.8 -> 65.0,
+        // 128 with offsets 67.1 -> 69.3.
+        constexpr bool WHOLE = EXPERTS && (GROUP == 32 || (GROUP == 128 && !BIAS));
 #pragma unroll
-        for (int b0 = 0; b0 < RB; b0 += PB) {
-          if (EXPERTS ? 16 * b0 >= rows : RB > PB && b0 >= size) break;
-          const uint32_t d = slot * L::W_SLOT + b0 * 1024, ds = take_s + slot * 2 * L::S_SLOT + b0 * 32;
+        for (int b = 0; b < RB; ++b) {
+          if (!WHOLE && (EXPERTS ? 16 * b >= rows : RB > 1 && b >= size)) break;
+          const uint32_t d = slot * L::W_SLOT + b * 1024, ds = take_s + slot * 2 * L::S_SLOT + b * 32;
 #pragma unroll
           for (int c = 0; c < CHUNKS; ++c) {
-            uint32_t u[PB][WPL], v[PB][WPL];
-            float2 s[PB], o[PB];
-#pragma unroll
-            for (int b = 0; b < PB; ++b) {
-              lds_words<WPL>(take[c] + d + b * 1024, u[b]);
-              lds_words<WPL>(take[c] + d + b * 1024 + 512, v[b]);
-            }
-#pragma unroll
-            for (int b = 0; b < PB; ++b) {
-              const uint32_t sa = ds + c * (2 * L::ROWS) + b * 32;
-              s[b] = make_float2(lds_half(sa), lds_half(sa + 16));
-              if (BIAS) o[b] = make_float2(lds_half(sa + L::S_SLOT), lds_half(sa + L::S_SLOT + 16));
-            }
-            float lo[PB][4], hi[PB][4];
+            uint32_t u[WPL], v[WPL];
+            lds_words<WPL>(take[c] + d, u);
+            lds_words<WPL>(take[c] + d + 512, v);
+            const uint32_t sa = ds + c * (2 * L::ROWS);
+            const float2 s = make_float2(lds_half(sa), lds_half(sa + 16));
+            float2 o = make_float2(0.0f, 0.0f);
+            if (BIAS) o = make_float2(lds_half(sa + L::S_SLOT), lds_half(sa + L::S_SLOT + 16));
+            float lo[4], hi[4];
 #pragma unroll
             for (int j = 0; j < WPL; ++j) {
               const uint2 p = xl[c * WPL + j], q = xh[c * WPL + j];
-#pragma unroll
-              for (int b = 0; b < PB; ++b) {
-                const uint4 uc = widen_word(u[b][j], wk), vc = widen_word(v[b][j], wk);
-                if (j == 0) {
-                  mma_f16_first(lo[b], uc.x, vc.x, uc.z, vc.z, p.x, p.y);
-                  mma_f16_first(hi[b], uc.y, vc.y, uc.w, vc.w, q.x, q.y);
-                } else {
-                  mma_f16(lo[b], uc.x, vc.x, uc.z, vc.z, p.x, p.y);
-                  mma_f16(hi[b], uc.y, vc.y, uc.w, vc.w, q.x, q.y);
-                }
+              const uint4 uc = widen_word(u[j], wk), vc = widen_word(v[j], wk);
+              if (j == 0) {
+                mma_f16_first(lo, uc.x, vc.x, uc.z, vc.z, p.x, p.y);
+                mma_f16_first(hi, uc.y, vc.y, uc.w, vc.w, q.x, q.y);
+              } else {
+                mma_f16(lo, uc.x, vc.x, uc.z, vc.z, p.x, p.y);
+                mma_f16(hi, uc.y, vc.y, uc.w, vc.w, q.x, q.y);
               }
             }
 #pragma unroll
-            for (int b = 0; b < PB; ++b)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {          // e & 1: token 2 t or 2 t + 1, e >> 1: channel g or g + 8
-                float& sum = acc[b0 + b][n][e];
-                sum = fmaf(e < 2 ? s[b].x : s[b].y, lo[b][e] + hi[b][e], sum);
-                if (BIAS) sum = fmaf(e < 2 ? o[b].x : o[b].y, (e & 1) ? sx[c].y : sx[c].x, sum);
-              }
+            for (int e = 0; e < 4; ++e) {              // e & 1: token 2 t or 2 t + 1, e >> 1: channel g or g + 8
+              float& sum = acc[b][n][e];
+              sum = fmaf(e < 2 ? s.x : s.y, lo[e] + hi[e], sum);
+              if (BIAS) sum = fmaf(e < 2 ? o.x : o.y, (e & 1) ? sx[c].y : sx[c].x, sum);
+            }
           }
         }
       }
