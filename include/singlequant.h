@@ -288,8 +288,11 @@ sq_status_t sq_linear_grouped(const sq_rotation_t* const* rots, int32_t E, const
  *   sg     fp16 [G x N], group-major: the scales of all channels of one group lie side by side
  *   bg     fp16 [G x N] or NULL (no offset).  A checkpoint with unsigned codes u and zero points z,
  *          w = s (u - z), has code = u - 8 (u ^ 8 as a nibble) and bg = s (8 - z).
- * sg and bg are finite and |code * sg + bg| < 65504: the kernels for more than 8 rows (16 of a small layer)
- * round each weight once to fp16 (one fused multiply-add), the others do not round it.  Sums are fp32.
+ * sg and bg are finite and |code * sg + bg| < 65504.  Sums are fp32.  Weights, with K % 32 == 0: the tensor-memory
+ * kernels round each of them once to fp16 (one fused multiply-add); they take dense calls of more than 16 rows, of
+ * 9 to 16 rows where N * K > 30e6, and of any rows where N is odd, and experts' calls where M > 8 * E or N is odd.
+ * All other calls, and all with K % 32 != 0, do not round weights: their products are those of the codes, scaled and
+ * offset group by group in fp32, with an error of fp32's steps of (|code| sg + |bg|) |Z16|.
  * A token with an infinity or a NaN gets infinities or NaN in its own row (which of them may differ from
  * kernel to kernel); the other rows do not depend on it.
  * ------------------------------------------------------------------------------------------- */
@@ -299,9 +302,10 @@ sq_status_t sq_linear_grouped(const sq_rotation_t* const* rots, int32_t E, const
  *   W             DEVICE fp16 [N x K], K == n of the handle, K % 8 == 0, K <= 32768
  *   bits          4 or 3
  *   Wq, sg        DEVICE (out)
- *   bg_or_null    NULL: symmetric, step = fp16(max|w| / (2^(bits-1) - 1)), code = clamp(floor(w / step + 1/2));
- *                 else DEVICE (out): step = fp16((max - min) / (2^bits - 1)), offset = fp16(min + 2^(bits-1) step),
- *                 code = clamp(floor((w - offset) / step + 1/2))
+ *   bg_or_null    NULL: symmetric, step = fp16(max|w| / (2^(bits-1) - 1)), offset = 0;
+ *                 else DEVICE (out): step = fp16((max - min) / (2^bits - 1)), offset = fp16(min + 2^(bits-1) step).
+ *                 code = clamp(floor(fl(fl(fl(w - offset) * fl(1/step)) + 0.5))) in fp32 arithmetic, as sq_pack_weight
+ *                 (a weight half a step from two codes may go to either); 0 where the step is 0
  *   workspace     DEVICE, sq_pack_weight_gs_workspace_bytes(N, K) bytes, 256-byte aligned; unused with NULL rot */
 size_t sq_pack_weight_gs_workspace_bytes(int64_t N, int64_t K);
 sq_status_t sq_pack_weight_gs(const sq_rotation_t* rot_or_null, const void* W, int64_t N, int64_t K, int32_t bits,

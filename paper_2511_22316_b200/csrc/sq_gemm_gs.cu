@@ -337,9 +337,9 @@ gs_stream_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
           __syncwarp();                              // the other lanes' scales
         }
         // A tile of experts has all its blocks of channels but for an expert's last (what lies behind the channels is not stored), and
-        // without a way out of the loop the compiler mixes the blocks: 16 tokens on eight experts, 4096 -> 14336, groups of 128 55.7 -> 53.8
-        // us (two blocks side by side: 57.4); groups of 32 71.9 -> 71.1, with offsets 86.8 -> 84.6.  The other forms run out of registers by it: groups of 64 63.8 -> 65.0,
-        // 128 with offsets 67.1 -> 69.3.
+        // without a way out of the loop the compiler mixes the blocks: 16 tokens on eight experts, 4096 -> 14336, groups of 128 55.7 -> 55.1
+        // us (two blocks side by side: 57.4); groups of 32 71.9 -> 67.8, with offsets 86.8 -> 82.5.  The other forms run out of registers by
+        // it: groups of 64 63.8 -> 65.0, 128 with offsets 67.1 -> 69.3.
         constexpr bool WHOLE = EXPERTS && (GROUP == 32 || (GROUP == 128 && !BIAS));
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
@@ -584,7 +584,8 @@ sq_status_t launch_stream(const GsArgs& a, cudaStream_t s) {
   if (a.E > 0) return launch_stream_any<true>(a, 1, 4, 1, slots, s);
   const int nt = a.M <= 8 ? 1 : 2, cap = nt == 1 ? 4 : 2;
   const int64_t nb = (a.N + 15) / 16;
-  // Time of a call in us, fitted to one to eight rows of five shapes, 4096 x 4096 to 8192 x 28672, with K in 1 to 8 parts (10 % off): a
+  // Time of a call in us, fitted to one to eight rows of five shapes, 4096 x 4096 to 8192 x 28672, with K in 1 to 8 parts (10 % off; the
+  // codes were subnormals then, see above, and the times have moved by -17 to +4 % since; the choices are those of the fit): a
   // step of 128 channels costs something by itself, something for its rows and something for its blocks of 16 channels, more with
   // small groups, and a third less where an SM has one block.  K over a cluster costs 1.5 us and has to fit the chip at once: 5 x
   // 14336 -> 4096 with K in 1 / 2 / 4 parts 16.2 / 12.5 / 12.4 us, but 17.7 with 74 clusters of four.

@@ -86,7 +86,10 @@ __device__ __forceinline__ uint4 widen_word(uint32_t word, const WidenConsts& k)
   return make_uint4(widen_low(word, k), widen_high(word, k), widen_low(w8, k), widen_high(w8, k));
 }
 
-// code * scale (+ offset) of a word's eight weights, pairs as widen_word leaves them.
+// code * scale (+ offset) of a word's eight weights, pairs as widen_word leaves them.  Each is rounded once to fp16, half a step of 2^-11:
+// a code's four bits and a scale's eleven do not fit the MMA's operand, and scaling behind each group's sums instead would read
+// the accumulator out of tensor memory for every 32 to 128 channels.  With the rounding of the result the error against 64 bits is 2.8e-4
+// to 3.1e-4 of the result's norm in place of 2.1e-4.
 template <bool BIAS>
 __device__ __forceinline__ uint4 scaled_word(uint32_t word, const WidenConsts& k, __half2 s, __half2 b) {
   const uint4 c = widen_word(word, k);

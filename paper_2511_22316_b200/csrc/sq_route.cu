@@ -8,8 +8,9 @@
 //   dl = p (d - sum_e p_e d_e),  d_e = c_e  (+ dgates_j where e is the token's j-th expert, gates over all experts)
 //   dl_{e_j} += g_j (dgates_j - sum_i g_i dgates_i)   (gates over the selected experts)
 //
-// Few tokens are bound by latency (16 tokens, 2 of 8 experts: 3.9 us), many by the instructions of softmax and selection (16384 tokens, 8
-// of 256 experts: 27 us, 0.4 TB/s; their gradient 11.6 us), the combination by memory (80 % of the copy rate).  A token belongs to LPT lanes of
+// Few tokens are bound by latency (16 tokens, 2 of 8 experts: 3.8 us), many by the instructions of softmax and selection (16384 tokens, 8
+// of 256 experts: 26.6 us, 0.4 TB/s; their gradient 11.3 us; graph replays), the combination by memory (80 % of the copy rate).  A token
+// belongs to LPT lanes of
 // a warp (8, 16 or 32), EPL neighbouring experts to each of them: a row is one vector load per lane, stays in registers, and
 // ties go to the lowest lane and so to the lowest index.  Every group of LPT lanes takes a contiguous run of tokens, and every
 // block a run of groups: the row that a slot gets is the number of slots of the same expert before it, and that is the sum of

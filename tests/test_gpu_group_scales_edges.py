@@ -100,3 +100,36 @@ def test_layer_in_front_of_every_kernel(M, N, offset):
     Y.check()
     check(Y.numpy(np.float16, (2 * M, N)), Z16.cpu().numpy()[rows], w)
     rot.close()
+
+
+@pytest.mark.parametrize("bits", [4, 3])
+@pytest.mark.parametrize("offset", [False, True])
+def test_weights_half_a_step_between_codes(bits, offset):
+    """The code is floor(fl(fl(fl(w - offset) * fl(1 / step)) + 1/2)) in fp32, as the header says, where a division would take another."""
+    top = (1 << (bits - 1)) - 1
+    maxima = np.arange(1, 2048, dtype=np.float32) / 4096
+    lo = np.float32(0.25) if offset else np.float32(0)
+    span = np.float32(2 * top + 1 if offset else top)
+    step = (maxima / span).astype(np.float16).astype(np.float32)
+    W = np.zeros((len(maxima), 32), np.float16)
+    for i, c in enumerate(np.arange(-top, top, dtype=np.float32)):
+        W[:, i] = (c + np.float32(0.5)) * step
+    if offset:
+        W += np.float16(0.25)
+    W[:, 30], W[:, 31] = (lo - maxima / 2, lo + maxima / 2) if offset else (0, maxima)
+    Wq, s, b = Guarded(W.size // 2), Guarded(len(W) * 2), Guarded(len(W) * 2)
+    sq.sq_pack_weight_gs(None, dev(W), len(W), 32, bits, 32, Wq, s, b if offset else None)
+    words = Wq.numpy(np.uint32, (len(W), 4))
+    codes = np.zeros(W.shape, np.int64)
+    for c in range(8):
+        codes[:, c::8] = (((words >> np.uint32(4 * sbo.POSITION[c])) & 15) ^ 8).astype(np.int64) - 8
+    f = W.astype(np.float32)
+    d = s.numpy(np.float16, (len(W), 1)).astype(np.float32)
+    o = b.numpy(np.float16, (len(W), 1)).astype(np.float32) if offset else np.float32(0)
+    with np.errstate(divide="ignore"):
+        inv = np.where(d > 0, np.float32(1) / d, np.float32(0))
+    want = np.clip(np.floor((f - o) * inv + np.float32(0.5)), -top - 1, top)
+    assert np.array_equal(codes, want)
+    # either neighbour is half a step away, 8 steps times 2^-22 for the reciprocal's and the product's roundings; the clamp cuts what the
+    # roundings of the step (half a step of fp16, 2^-11, over a range of 2 (top + 1) of them) and of the offset (2^-11 of it) leave outside
+    assert np.all(np.abs(f - o - codes * d) <= d * (0.5 + 8 * 2.0 ** -22) + (top + 1) * d * 2.0 ** -10 + np.abs(o) * 2.0 ** -11 + 2.0 ** -25)
