@@ -133,3 +133,49 @@ def test_weights_half_a_step_between_codes(bits, offset):
     # either neighbour is half a step away, 8 steps times 2^-22 for the reciprocal's and the product's roundings; the clamp cuts what the
     # roundings of the step (half a step of fp16, 2^-11, over a range of 2 (top + 1) of them) and of the offset (2^-11 of it) leave outside
     assert np.all(np.abs(f - o - codes * d) <= d * (0.5 + 8 * 2.0 ** -22) + (top + 1) * d * 2.0 ** -10 + np.abs(o) * 2.0 ** -11 + 2.0 ** -25)
+
+
+def test_products_on_two_streams_at_once():
+    """A call of every kernel, beside another one on a stream and in a workspace of its own: the bits of calls one by one."""
+    import torch
+    N, K, group, E = 512, 1024, 64, 6
+    rng = np.random.default_rng(1)
+    codes, sg, bg = make_weights(rng, N, K, group, True)
+    Wq, s, b = dev(sbo.pack_codes(codes)), dev(sg), dev(bg)
+    many = lambda t: torch.stack([t.roll(e, 0) for e in range(E)])
+    WqE, sE, bE = many(Wq), many(s), many(b)
+
+    class Call:
+        def __init__(self, M, per):
+            rows = E * per
+            self.M, self.rows = M, rows
+            self.Z = dev(rng.standard_normal((M, K)).astype(np.float16))
+            self.token = dev(rng.integers(0, M, rows).astype(np.int32))
+            self.offsets = dev((np.arange(E + 1) * per).astype(np.int32))
+            self.nb = sq.sq_gemm_gs_grouped_workspace_bytes(rows, K)
+            self.ws = torch.empty(self.nb, dtype=torch.uint8, device="cuda")
+            self.Y, self.YE = (torch.zeros(n, N, dtype=torch.float16, device="cuda") for n in (M, rows))
+
+        def run(self):
+            sq.sq_w4a16_gemm_gs(self.Z, Wq, s, b, self.M, N, K, group, self.Y)
+            sq.sq_w4a16_gemm_gs_grouped(self.Z, self.M, self.token, self.offsets, E, WqE, sE, bE, self.rows, N, K, group, self.ws, self.nb, self.YE)
+
+    calls = [Call(M, per) for M, per in ((1, 3), (5, 40), (16, 8), (30, 20), (64, 2), (300, 100))]
+    torch.cuda.synchronize()
+    want = []
+    for c in calls:
+        c.run()
+        torch.cuda.synchronize()
+        want.append((c.Y.clone(), c.YE.clone()))
+        c.Y.zero_()
+        c.YE.zero_()
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(30):
+        for c, st in zip(calls, streams):
+            with torch.cuda.stream(st):
+                c.run()
+    torch.cuda.synchronize()
+    assert sq.sq_last_device_status() == sq.SQ_OK
+    for c, (Y, YE) in zip(calls, want):
+        assert torch.equal(c.Y, Y) and torch.equal(c.YE, YE)

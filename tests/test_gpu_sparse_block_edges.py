@@ -64,3 +64,66 @@ def test_loss_of_many_tokens(T, E):
     # 1 / E once; 64 additions in a register, one for each 64 tokens, at most 24 over the groups of a block, 10 over the blocks; the result
     roundings = 1 + 64 + run // 64 + 1 + 24 + 10 + 1
     assert abs(loss.item() - 1) <= roundings * 2.0 ** -24 * (1 + 2.0 ** -10)
+
+
+class Gradients:
+    """Router, its gradient, the combination and its gradient on buffers that stay."""
+
+    def __init__(self, T, E, k, N):
+        import torch
+        z = lambda *s, t=torch.float32: torch.zeros(*s, dtype=t, device="cuda")
+        self.T, self.E, self.k, self.N = T, E, k, N
+        self.x, self.Y, self.dout, self.dl = z(T, E), z(T * k, N, t=torch.float16), z(T, N, t=torch.float16), z(1)
+        i32 = torch.int32
+        self.ids, self.pos, self.rows, self.counts, self.offsets = z(T, k, t=i32), z(T, k, t=i32), z(T * k, t=i32), z(E + 1, t=i32), z(E + 1, t=i32)
+        self.gates, self.loss, self.out, self.dY, self.dg, self.dx = z(T, k), z(1), z(T, N, t=torch.float16), z(T * k, N, t=torch.float16), z(T, k), z(T, E)
+        self.nb = sq.sq_route_workspace_bytes(T, E)
+        self.ws = z(max(256, self.nb), t=torch.uint8)
+
+    def fill(self, seed):
+        import torch
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        for t in (self.x, self.Y, self.dout, self.dl):
+            t.copy_(torch.randn(t.shape, device="cuda", generator=g))
+
+    def step(self):
+        T, E, k, N, M = self.T, self.E, self.k, self.N, self.T * self.k
+        sq.sq_route(self.x, sq.SQ_F32, T, E, E, k, 1, None, self.ids, self.gates, self.counts, self.offsets, self.rows, self.pos, self.loss, self.ws, self.nb)
+        sq.sq_combine(self.Y, M, self.pos, self.gates, T, k, N, self.out)
+        sq.sq_combine_backward(self.dout, self.Y, M, self.pos, self.gates, T, k, N, self.dY, self.dg)
+        sq.sq_route_backward(self.x, sq.SQ_F32, T, E, E, k, 1, None, self.ids, self.gates, self.counts, self.dg, self.dl, self.dx, E)
+
+    def results(self):
+        import torch
+        torch.cuda.synchronize()
+        return [t.clone() for t in (self.ids, self.pos, self.rows, self.counts, self.offsets, self.gates, self.loss, self.out, self.dY, self.dg, self.dx)]
+
+
+@pytest.mark.parametrize("T,E,k,N", [(5, 8, 2, 64), (700, 60, 4, 520), (10000, 40, 2, 64)])
+def test_gradients_captured_and_on_two_streams_at_once(T, E, k, N):
+    """Bits of a replay on other inputs, and of two of them on streams of their own at the same time, are those of calls one by one."""
+    import torch
+    one, want = Gradients(T, E, k, N), {}
+    for seed in (1, 2, 3):
+        one.fill(seed)
+        one.step()
+        want[seed] = one.results()
+    both = [Gradients(T, E, k, N), Gradients(T, E, k, N)]
+    streams, graphs = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for g, s in zip(both, streams):
+        g.fill(1)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            g.step()
+        graphs.append(graph)
+    for first, second in ((2, 3), (3, 1)):
+        both[0].fill(first)
+        both[1].fill(second)
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for graph, s in zip(graphs, streams):
+                with torch.cuda.stream(s):
+                    graph.replay()
+        for g, seed in zip(both, (first, second)):
+            assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(g.results(), want[seed]))
